@@ -233,6 +233,96 @@ flowmm_status flowmm_cache_remerge(const flowmm_params *p, const int32_t *cu_cap
                                    const flowmm_plan_buffers *plan, void *workspace, size_t workspace_bytes,
                                    void *stream);
 
+/* ---- attention with scored and masked logits; the compacted cache in 8 bits ---------------------
+ * What follows is what a model needs around the merged cache: the prompt's own attention, and a
+ * decode step over a cache that has grown past its merged rows, as it is or held in 8 bits.  The
+ * logits may be capped and fall with distance (flowmm_scoring).  All arrays named "host" are read during the
+ * call only, so a captured call replays with the values it was captured with.  As everywhere, the
+ * stream's device must be the current one. */
+
+/* How an attention call makes scores of logits; NULL in its place, or all zeros: plain attention.
+ * For query head h, the query at position i and the key at position j of its sequence:
+ *   x = scale * <q, k>;  cap > 0: x = cap * tanh(x / cap);  slopes: x = x - slopes[h] * |i - j|.
+ * prefix and image_spans are read by flowmm_prompt_attention, row_pos and q_pos by the two cache
+ * attentions (which need both or neither). */
+typedef struct {
+  float cap;              /* finite, >= 0; 0: no cap */
+  const float *slopes;    /* device [Hq], or NULL: no bias */
+  const int32_t *prefix;  /* host [batch], 0 <= prefix[b] <= L_b, or NULL: the first prefix[b] tokens of sequence b see each other */
+  int32_t image_spans;    /* not 0: an image token sees its whole span */
+  const int32_t *row_pos; /* device [Lyr][Hkv][SB] as kept_idx: position of merged row r < B_b of sequence b at [its first slot + r];
+                             the rows behind them are the sequence's last tokens, ending at q_pos[b] (len_b - 1 - r before it) */
+  const int32_t *q_pos;   /* host [batch]: position of the query.  Without the two: row r has position r, the query that of the last row */
+} flowmm_scoring;
+
+/* The prompt's attention (the attention of the paper's Preliminary section with every token as a query):
+ *   out[l][h][t] = sum_j softmax_j(x_tj) V[l][kv(h)][j]
+ * over the keys j that token t of its sequence sees: all up to itself, and where the scoring says so
+ * all of the prefix (t in it) or of its image span.  The sequences of the batch do not see each
+ * other.  K, V through p's k strides; Q_full and out [Lyr][Hq][T][d] through the three
+ * strides given (as for flowmm_flow_exact); out must not overlap the inputs.  The weights of bf16 calls are
+ * rounded to bf16 for the product with V (their sum is not), the sums are fp32.  p, workspace (size from flowmm_plan_sizes),
+ * stream and errors as for flowmm_plan; window, budgets, tau and theta are validated but not used. */
+flowmm_status flowmm_prompt_attention(const flowmm_params *p, const flowmm_scoring *scoring, const void *K, const void *V,
+                                      const void *Q_full, int64_t qf_stride_layer, int64_t qf_stride_head,
+                                      int64_t qf_stride_token, void *out, void *workspace, size_t workspace_bytes,
+                                      void *stream);
+
+/* In the calls below p, cu_capacity and lengths describe the cache as they do for flowmm_cache_append
+ * (of p: n_layers, n_q_heads, n_kv_heads, head_dim, dtype, batch, k_stride_*; scale for the attentions; budget_tokens,
+ * 0 < B_b <= C_b, only where row_pos is given).  A sequence of length 0 is left alone; its attention is 0. */
+
+/* One decode step of attention over a cache with head room: for every layer l, query head h and sequence b
+ *   out[l][h][b] = sum_r softmax_r(x_r) V_c[l][kv(h)][cu_capacity[b] + r],   r < lengths[b],
+ * q, out [Lyr][Hq][batch][d] contiguous, dtype of the cache.  32 consecutive rows must lie within 4 GiB
+ * (FLOWMM_EUNSUPPORTED otherwise).  Rows from lengths[b] on are not read. */
+flowmm_status flowmm_cache_attention(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                     const flowmm_scoring *scoring, const void *q, const void *K_c, const void *V_c,
+                                     void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A cache in 8 bits: codes are e4m3 numbers (OCP: 1 + 4 + 3 bits, no infinity, +-448 the largest), one
+ * a channel; FLOWMM_QUANT_ROWS consecutive rows of a sequence (counted from the start of its range) share an
+ * fp32 scale per (layer, kv head), K and V each their own; a row is code * scale.  flowmm_cache_quantize and
+ * flowmm_cache_append_quantized write powers of two, the readers take any finite scale. */
+enum { FLOWMM_QUANT_ROWS = 32 };
+typedef struct {
+  void *k_codes, *v_codes;   /* device: element (l, g, row, c) at l*stride_layer + g*stride_head + row*stride_token + c */
+  float *k_scales, *v_scales; /* device [Lyr][Hkv][NB] contiguous, NB = sum over b of ceil(C_b / FLOWMM_QUANT_ROWS), sequence after sequence */
+  int64_t stride_layer, stride_head, stride_token; /* bytes, multiples of 16, stride_token >= head_dim */
+} flowmm_quantized_cache;
+
+/* Bytes of k_codes (as of v_codes) when contiguous, of k_scales (as of v_scales), and of the workspace of the two cache attentions at
+ * whatever lengths.  Any pointer may be NULL.  Pure host computation. */
+flowmm_status flowmm_cache_sizes(const flowmm_params *p, const int32_t *cu_capacity, size_t *codes_bytes, size_t *scales_bytes,
+                                 size_t *workspace_bytes);
+
+/* The first lengths[b] rows of every sequence into 8 bits.  They lie at token cu_rows[b] (host [batch], >= 0; not
+ * necessarily ascending) of K_rows / V_rows, which p's k strides address: the outputs of flowmm_merge with the budgets'
+ * prefix sums, or a cache with cu_capacity itself.  A block's scale is the smallest power of two, 2^-120 at the least, that
+ * brings its largest finite number within 448; codes are rounded to nearest-even, infinities become
+ * +-448, NaN stays NaN.  Rows and scales behind the lengths[b] are left as they were. */
+flowmm_status flowmm_cache_quantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                    const int32_t *cu_rows, const void *K_rows, const void *V_rows,
+                                    const flowmm_quantized_cache *cache, void *stream);
+
+/* The way back, for a re-merge: rows code * scale, rounded to nearest-even in the dtype of p. */
+flowmm_status flowmm_cache_dequantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                      const int32_t *cu_rows, const flowmm_quantized_cache *cache, void *K_rows,
+                                      void *V_rows, void *stream);
+
+/* flowmm_cache_append for a cache in 8 bits: row lengths[b] becomes k_new / v_new [Lyr][Hkv][batch][d] (contiguous, dtype of p).
+ * The first row of a block sets the block's scale as flowmm_cache_quantize would; a later row that needs a larger one raises it,
+ * and the block's older codes become e4m3(code * old scale / new scale), nearest-even. */
+flowmm_status flowmm_cache_append_quantized(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                            const flowmm_quantized_cache *cache, const void *k_new, const void *v_new,
+                                            void *stream);
+
+/* flowmm_cache_attention over a cache in 8 bits; q and out have the dtype of p. */
+flowmm_status flowmm_cache_attention_quantized(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                               const flowmm_scoring *scoring, const void *q,
+                                               const flowmm_quantized_cache *cache, void *out, void *workspace,
+                                               size_t workspace_bytes, void *stream);
+
 /* Message of the last failing call on this thread (static storage, never NULL). */
 const char *flowmm_last_error(void);
 

@@ -27,6 +27,8 @@ EXPORTS = ("flowmm_plan_sizes", "flowmm_plan", "flowmm_merge", "flowmm_plan_merg
            "flowmm_static_workspace_bytes", "flowmm_flow_exact",
            "flowmm_cache_append", "flowmm_cache_remerge_sizes", "flowmm_cache_remerge",
            "flowmm_decode_attention", "flowmm_last_error",
+           "flowmm_cache_sizes", "flowmm_cache_quantize", "flowmm_cache_dequantize", "flowmm_cache_append_quantized",
+           "flowmm_cache_attention", "flowmm_cache_attention_quantized", "flowmm_prompt_attention",
            "flowmm_profile_kernel_count", "flowmm_profile_kernel_name", "flowmm_profile_select",
            "flowmm_profile_collect")
 
@@ -51,6 +53,19 @@ class flowmm_params(C.Structure):
 
 class flowmm_plan_buffers(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in PLAN_FIELDS]
+
+
+FLOWMM_QUANT_ROWS = 32  # rows of a cache in 8 bits that share a scale
+
+
+class flowmm_scoring(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("prefix", C.POINTER(C.c_int32)), ("image_spans", C.c_int32),
+                ("row_pos", C.c_void_p), ("q_pos", C.POINTER(C.c_int32))]
+
+
+class flowmm_quantized_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("stride_layer", C.c_int64), ("stride_head", C.c_int64), ("stride_token", C.c_int64)]
 
 
 class FlowMMError(RuntimeError):
@@ -94,6 +109,8 @@ def load(build_if_missing: bool = True):
         lib.flowmm_flow_exact.argtypes = [C.POINTER(flowmm_params), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64,
                                           C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.flowmm_flow_exact.restype = C.c_int
+        lib.flowmm_cache_sizes.argtypes = [C.POINTER(flowmm_params), i32p, *[C.POINTER(C.c_size_t)] * 3]
+        lib.flowmm_cache_sizes.restype = C.c_int
         for f in (lib.flowmm_plan_sizes, lib.flowmm_profile_collect, lib.flowmm_profile_kernel_count):
             f.restype = C.c_int
         lib.flowmm_profile_kernel_name.restype = C.c_char_p
@@ -235,6 +252,93 @@ def flowmm_decode_attention(params: Params, q: int, K_c: int, V_c: int, out: int
     _check(_native().decode_attention(C.addressof(params.c), q, K_c, V_c, out, workspace, workspace_bytes, stream))
 
 
+class Scoring:
+    """Owns the host arrays a flowmm_scoring points to.  slopes and row_pos are device addresses (0: none), prefix and q_pos
+    integers per sequence."""
+
+    def __init__(self, cap: float = 0.0, slopes: int = 0, prefix=None, image_spans: bool = False, row_pos: int = 0, q_pos=None):
+        self._prefix, prefix_p = (None, None) if prefix is None else _i32_array(prefix)
+        self._q_pos, q_pos_p = (None, None) if q_pos is None else _i32_array(q_pos)
+        self.c = flowmm_scoring(float(cap), slopes or None, prefix_p, int(bool(image_spans)), row_pos or None, q_pos_p)
+
+    def address(self, batch: int) -> int:
+        """Address of the structure for a call on `batch` sequences: shorter arrays are refused here, the library gets no count."""
+        for name, a in (("prefix", self._prefix), ("q_pos", self._q_pos)):
+            if a is not None and a.size < batch:
+                raise ValueError(f"{name} has {a.size} entries, {batch} expected")
+        return C.addressof(self.c)
+
+
+def _scoring(scoring: Scoring | None, params: Params):
+    return None if scoring is None else scoring.address(params.batch)
+
+
+def flowmm_cache_sizes(params: Params, cu_capacity) -> Tuple[int, int, int]:
+    """Bytes of a cache's codes and of its scales (K's, or V's) in 8 bits, and of the cache attentions' workspace."""
+    cap, cap_p = _i32_array(cu_capacity)
+    if cap.size < params.batch + 1:
+        raise ValueError(f"cu_capacity has {cap.size} entries, {params.batch + 1} expected")
+    n = [C.c_size_t(0) for _ in range(3)]
+    _check(load().flowmm_cache_sizes(C.byref(params.c), cap_p, *[C.byref(x) for x in n]))
+    return tuple(int(x.value) for x in n)
+
+
+class QuantizedCache:
+    """A cache in 8 bits: codes [Lyr][Hkv][rows][d] (torch.float8_e4m3fn) and scales [Lyr][Hkv][blocks] (fp32) of K and of V, allocated with
+    torch on `device` or taken from `tensors` (k_codes, v_codes, k_scales, v_scales; of the codes the last dimension is contiguous, the scales are)."""
+
+    def __init__(self, params: Params, cu_capacity, device="cuda:0", tensors=None):
+        import torch
+        blocks = flowmm_cache_sizes(params, cu_capacity)[1] // (4 * params.n_layers * params.n_kv_heads)
+        unit = (params.n_layers, params.n_kv_heads)
+        codes, scales = (*unit, int(_i32_array(cu_capacity)[0].reshape(-1)[params.batch]), params.head_dim), (*unit, blocks)
+        if tensors is None:
+            tensors = [torch.zeros(codes, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+            tensors += [torch.zeros(scales, dtype=torch.float32, device=device) for _ in range(2)]
+        k, v, ks, vs = tensors
+        for t, shape, dtype in ((k, codes, torch.float8_e4m3fn), (v, codes, torch.float8_e4m3fn), (ks, scales, torch.float32), (vs, scales, torch.float32)):
+            if tuple(t.shape) != shape or t.dtype != dtype:
+                raise ValueError(f"a {dtype} tensor of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
+        if k.stride() != v.stride() or k.stride(-1) != 1 or not ks.is_contiguous() or not vs.is_contiguous():
+            raise ValueError("k_codes and v_codes share their strides, their last dimension and the scales are contiguous")
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k, v, ks, vs
+        self.c = flowmm_quantized_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), *k.stride()[:3])
+
+
+def flowmm_cache_quantize(params: Params, cu_capacity, lengths, cu_rows, K: int, V: int, cache: QuantizedCache, stream: int = 0):
+    """The first `lengths[b]` rows of every sequence, from token `cu_rows[b]` of K and V on, into 8 bits."""
+    _check(_native().cache_quantize(C.addressof(params.c), cu_capacity, lengths, cu_rows, K, V, C.addressof(cache.c), 0, stream))
+
+
+def flowmm_cache_dequantize(params: Params, cu_capacity, lengths, cu_rows, cache: QuantizedCache, K: int, V: int, stream: int = 0):
+    """The way back: rows of the dtype of `params`, as a re-merge takes them."""
+    _check(_native().cache_quantize(C.addressof(params.c), cu_capacity, lengths, cu_rows, K, V, C.addressof(cache.c), 1, stream))
+
+
+def flowmm_cache_append_quantized(params: Params, cu_capacity, lengths, cache: QuantizedCache, k_new: int, v_new: int, stream: int = 0):
+    """One new K/V row per sequence behind its `lengths[b]` valid ones, in 8 bits."""
+    _check(_native().cache_append_quantized(C.addressof(params.c), cu_capacity, lengths, C.addressof(cache.c), k_new, v_new, stream))
+
+
+def flowmm_cache_attention(params: Params, cu_capacity, lengths, scoring: Scoring | None, q: int, K_c: int, V_c: int, out: int, workspace: int,
+                           workspace_bytes: int, stream: int = 0):
+    """One decode step of attention over the valid rows of a cache with head room."""
+    _check(_native().cache_attention(C.addressof(params.c), cu_capacity, lengths, _scoring(scoring, params), q, K_c, V_c, out, workspace, workspace_bytes,
+                                     stream))
+
+
+def flowmm_cache_attention_quantized(params: Params, cu_capacity, lengths, scoring: Scoring | None, q: int, cache: QuantizedCache, out: int,
+                                     workspace: int, workspace_bytes: int, stream: int = 0):
+    _check(_native().cache_attention_quantized(C.addressof(params.c), cu_capacity, lengths, _scoring(scoring, params), q, C.addressof(cache.c), out,
+                                               workspace, workspace_bytes, stream))
+
+
+def flowmm_prompt_attention(params: Params, scoring: Scoring | None, K: int, V: int, Q_full: int, q_strides: Tuple[int, int, int], out: int,
+                            workspace: int, workspace_bytes: int, stream: int = 0):
+    """Attention of every prompt token; `out` is laid out as `Q_full`."""
+    _check(_native().prompt_attention(C.addressof(params.c), _scoring(scoring, params), K, V, Q_full, *q_strides, out, workspace, workspace_bytes, stream))
+
+
 def flowmm_profile_select(names: str = ""):
     load().flowmm_profile_select(names.encode())
 
@@ -315,6 +419,12 @@ class DeviceBuffers:
         K_c = self.K_out if K_c is None else K_c
         V_c = self.V_out if V_c is None else V_c
         flowmm_decode_attention(self.params, q.data_ptr(), K_c.data_ptr(), V_c.data_ptr(), out.data_ptr(),
+                                self.workspace.data_ptr(), self.workspace_bytes, stream)
+
+    def prompt_attention(self, K, V, Q_full, out, scoring: Scoring | None = None, stream: int = 0):
+        """Q_full, out [Lyr][Hq][T][d] contiguous."""
+        Hq, T, d = Q_full.shape[1:]
+        flowmm_prompt_attention(self.params, scoring, K.data_ptr(), V.data_ptr(), Q_full.data_ptr(), (Hq * T * d, T * d, d), out.data_ptr(),
                                 self.workspace.data_ptr(), self.workspace_bytes, stream)
 
     def merge(self, K, V, stream: int = 0):

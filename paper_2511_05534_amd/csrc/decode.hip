@@ -17,7 +17,7 @@
 #include <cfloat>
 #include <cstring>
 
-#include "device_common.h"
+#include "decode_core.h"
 #include "kernels.h"
 #include "profile.h"
 
@@ -28,16 +28,6 @@ namespace {
 constexpr int kDecodeTail = 1024;  // four per compute unit (512: 0 to 3 us slower, 2048 to all: 0 to 9)
 constexpr int kDThreads = 256;
 constexpr int kDWaves = kDThreads / 64;
-
-// (m, z, acc) <- fold of two partial softmax states of the same query head
-__device__ __forceinline__ void fold_state(float &m, float &z, float *acc, int n, float m2, float z2, const float *acc2) {
-  const float M = fmaxf(m, m2);
-  const float Ms = M == -INFINITY ? 0.f : M;
-  const float s1 = fast_exp2(m - Ms), s2 = fast_exp2(m2 - Ms);
-  z = z * s1 + z2 * s2;
-  for (int e = 0; e < n; ++e) acc[e] = acc[e] * s1 + acc2[e] * s2;
-  m = M;
-}
 
 // The last sequence of the launch, lo .. hi - 1, whose task number from bit SHIFT on is not behind i.
 template <int SHIFT>
@@ -245,10 +235,6 @@ constexpr int kMWaves = 8;   // waves of a workgroup, or fewer (decode_waves)
 constexpr int kMRows = 16;   // rows of a tile
 constexpr int kMHeads = 16;  // query heads of a kv group per launch
 
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-
 // the 16 rows r0 .. r0+15 (clamped to last) of src into a tile buffer, chunk c of row r at slot c ^ (r % NCH)
 template <int NCH>
 __device__ __forceinline__ void request_tile(const uint4 *src, int r0, int last, uint4 *tile) {
@@ -259,26 +245,6 @@ __device__ __forceinline__ void request_tile(const uint4 *src, int r0, int last,
     const int r = j * RPI + lane / NCH, ch = (lane % NCH) ^ (r % NCH);
     load_to_lds<16>(src, ((unsigned)min(r0 + r, last) * NCH + ch) * 16u, tile + j * 64);
   }
-}
-
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-// maximum over the lanes l, l^16, l^32, l^48
-__device__ __forceinline__ float quad_max(float v) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
 template <int D, int WAVES, bool ORDERED>

@@ -848,3 +848,297 @@ FLOWMM_API flowmm_status flowmm_cache_remerge(const flowmm_params *p, const int3
 }
 
 }  // extern "C"
+
+namespace {
+
+// ---- attention with scored and masked logits; the cache in 8 bits ---------------------------------------
+flowmm_status check_scoring(const flowmm_scoring *scoring, float scale, ScoreArgs &out) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  out = ScoreArgs{scale * kLog2e, 0.f, 0.f, nullptr};
+  if (!scoring) return FLOWMM_OK;
+  const float cap = scoring->cap;
+  if (!(cap >= 0.f) || !std::isfinite(cap * kLog2e)) return fail(FLOWMM_EINVAL, "cap must be finite and >= 0");
+  if (cap > 0.f) {
+    out.cap = cap * kLog2e;
+    out.cap_in = scale / cap;
+    if (!std::isfinite(out.cap_in)) return fail(FLOWMM_EINVAL, "cap is too small for the scale");
+  }
+  if (reinterpret_cast<uintptr_t>(scoring->slopes) & 3) return fail(FLOWMM_EINVAL, "slopes is not 4-byte aligned");
+  out.slopes = scoring->slopes;
+  return FLOWMM_OK;
+}
+
+float scale_of(const flowmm_params *p) { return p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->head_dim); }
+
+// what every call on a cache with head room checks of p, the ranges and the lengths
+flowmm_status check_cache(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths) {
+  flowmm_status st = check_cache_ranges(p, cu_capacity);
+  if (st != FLOWMM_OK) return st;
+  if (p->n_layers < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1) return fail(FLOWMM_EINVAL, "n_layers, n_q_heads and n_kv_heads must be >= 1");
+  if (p->n_q_heads % p->n_kv_heads != 0) return fail(FLOWMM_EINVAL, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads);
+  if (p->dtype != FLOWMM_F32 && p->dtype != FLOWMM_BF16) return fail(FLOWMM_EINVAL, "dtype must be FLOWMM_F32 or FLOWMM_BF16");
+  if (p->head_dim != 64 && p->head_dim != 128) return fail(FLOWMM_EUNSUPPORTED, "head_dim %d is not built (64 and 128 are)", p->head_dim);
+  if (p->n_q_heads > 1024 || p->n_layers > 65535) return fail(FLOWMM_EUNSUPPORTED, "more than 1024 query heads or 65535 layers");
+  if (!lengths) return FLOWMM_OK;
+  for (int b = 0; b < p->batch; ++b) {
+    const int cap = cu_capacity[b + 1] - cu_capacity[b];
+    if (lengths[b] < 0 || lengths[b] > cap) return fail(FLOWMM_EINVAL, "lengths[%d] = %d is outside [0, capacity=%d]", b, lengths[b], cap);
+  }
+  return FLOWMM_OK;
+}
+
+flowmm_status check_k_strides(const flowmm_params *p) {
+  const int epc = p->dtype == FLOWMM_BF16 ? 8 : 4;
+  const int64_t strides[3] = {p->k_stride_layer, p->k_stride_head, p->k_stride_token};
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < 0 || strides[i] % epc != 0) return fail(FLOWMM_EINVAL, "strides must be non-negative multiples of 16 bytes (%d elements)", epc);
+  if (p->k_stride_token < p->head_dim) return fail(FLOWMM_EINVAL, "token strides must be at least head_dim");
+  return FLOWMM_OK;
+}
+
+flowmm_status check_quantized(const flowmm_params *p, const flowmm_quantized_cache *c) {
+  if (!c) return fail(FLOWMM_EINVAL, "cache is NULL");
+  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return fail(FLOWMM_EINVAL, "k_codes, v_codes, k_scales and v_scales must not be NULL");
+  if (misaligned(c->k_codes) || misaligned(c->v_codes)) return fail(FLOWMM_EINVAL, "k_codes and v_codes must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(c->k_scales) | reinterpret_cast<uintptr_t>(c->v_scales)) & 3) return fail(FLOWMM_EINVAL, "k_scales and v_scales must be 4-byte aligned");
+  const int64_t strides[3] = {c->stride_layer, c->stride_head, c->stride_token};
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < 0 || strides[i] % 16 != 0) return fail(FLOWMM_EINVAL, "the strides of the codes must be non-negative multiples of 16 bytes");
+  if (c->stride_token < p->head_dim) return fail(FLOWMM_EINVAL, "the token stride of the codes must be at least head_dim");
+  return FLOWMM_OK;
+}
+
+// scales of a (layer, kv head)
+long long quant_blocks(const flowmm_params *p, const int32_t *cu_capacity) {
+  long long n = 0;
+  for (int b = 0; b < p->batch; ++b) n += ((long long)cu_capacity[b + 1] - cu_capacity[b] + kQuantRows - 1) / kQuantRows;
+  return n;
+}
+
+// Partial states of the cache attention, at whatever lengths within the capacities (rows_of_task keeps to this).
+size_t cache_attention_bytes(const flowmm_params *p, const int32_t *cu_capacity) {
+  const long long units = (long long)p->n_layers * p->n_kv_heads;
+  long long parts = 0;
+  for (int b = 0; b < p->batch; ++b) {
+    const long long n = ((long long)cu_capacity[b + 1] - cu_capacity[b] + kCacheAttnLeastPart - 1) / kCacheAttnLeastPart;
+    parts += n < kCacheAttnMostParts ? n : kCacheAttnMostParts;
+  }
+  const long long most = kCacheAttnTasks / units + p->batch;
+  if (parts > most) parts = most;
+  return align256((size_t)p->n_layers * p->n_q_heads * parts * (p->head_dim + 2) * 4);
+}
+
+flowmm_status quantize_call(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths, const int32_t *cu_rows, const void *K_rows,
+                            const void *V_rows, const flowmm_quantized_cache *cache, bool back, void *stream) {
+  flowmm_status st = check_cache(p, cu_capacity, lengths);
+  if (st != FLOWMM_OK) return st;
+  if (!lengths || !cu_rows) return fail(FLOWMM_EINVAL, "lengths and cu_rows must not be NULL");
+  for (int b = 0; b < p->batch; ++b)
+    if (cu_rows[b] < 0) return fail(FLOWMM_EINVAL, "cu_rows[%d] is negative", b);
+  if ((st = check_k_strides(p)) != FLOWMM_OK || (st = check_quantized(p, cache)) != FLOWMM_OK) return st;
+  if (!K_rows || !V_rows) return fail(FLOWMM_EINVAL, "K_rows and V_rows must not be NULL");
+  if (misaligned(K_rows) || misaligned(V_rows)) return fail(FLOWMM_EINVAL, "K_rows and V_rows must be 16-byte aligned");
+  if (p->n_kv_heads > 32767) return fail(FLOWMM_EUNSUPPORTED, "more than 32767 kv heads");
+  const int epc = p->dtype == FLOWMM_BF16 ? 8 : 4;
+  QuantArgs a;
+  a.K_rows = K_rows; a.V_rows = V_rows;
+  a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scales = cache->k_scales; a.v_scales = cache->v_scales;
+  a.ks_layer = p->k_stride_layer / epc; a.ks_head = p->k_stride_head / epc; a.ks_tok = p->k_stride_token / epc;
+  a.cs_layer = cache->stride_layer; a.cs_head = cache->stride_head; a.cs_tok = cache->stride_token;
+  a.Hkv = p->n_kv_heads;
+  a.NB = (int)quant_blocks(p, cu_capacity);
+  QuantCall c{cu_capacity, lengths, cu_rows, p->batch, p->n_layers, p->head_dim, p->dtype == FLOWMM_BF16, back};
+  const hipError_t e = launch_cache_quantize(a, c, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, back ? "cache dequantize kernel" : "cache quantize kernel");
+  return FLOWMM_OK;
+}
+
+// what the two cache attentions have in common; a.K_c .. and the strides are set
+flowmm_status cache_attention_call(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths, const flowmm_scoring *scoring, const void *q,
+                                   void *out, void *workspace, size_t workspace_bytes, CacheAttnArgs &a, RowKind rows, void *stream) {
+  if (!q || !out || !workspace) return fail(FLOWMM_EINVAL, "q, out and workspace must not be NULL");
+  if (misaligned(q) || misaligned(out) || misaligned(workspace)) return fail(FLOWMM_EINVAL, "q, out and workspace must be 16-byte aligned");
+  const size_t q_bytes = (size_t)p->n_layers * p->n_q_heads * p->batch * p->head_dim * (p->dtype == FLOWMM_BF16 ? 2 : 4);
+  if (overlaps(q, q_bytes, out, q_bytes)) return fail(FLOWMM_EINVAL, "out must not overlap q");
+  if (!(p->scale >= 0.f) || !std::isfinite(p->scale)) return fail(FLOWMM_EINVAL, "scale must be finite and >= 0");
+  if ((31 * a.ks_tok + p->head_dim) * 16 >= 1ll << 32) return fail(FLOWMM_EUNSUPPORTED, "32 cache rows span 4 GiB or more");
+  const flowmm_status st = check_scoring(scoring, scale_of(p), a.score);
+  if (st != FLOWMM_OK) return st;
+  a.row_pos = nullptr;
+  const int32_t *q_pos = scoring ? scoring->q_pos : nullptr;
+  if (scoring && (!scoring->row_pos != !q_pos)) return fail(FLOWMM_EINVAL, "row_pos and q_pos go together");
+  if (q_pos) {
+    if (reinterpret_cast<uintptr_t>(scoring->row_pos) & 3) return fail(FLOWMM_EINVAL, "row_pos is not 4-byte aligned");
+    if (!p->budget_tokens) return fail(FLOWMM_EINVAL, "row_pos needs budget_tokens");
+    for (int b = 0; b < p->batch; ++b) {
+      const int cap = cu_capacity[b + 1] - cu_capacity[b], B = p->budget_tokens[b];
+      if (B < 1 || B > cap) return fail(FLOWMM_EINVAL, "budget %d of sequence %d is outside [1, capacity=%d]", B, b, cap);
+    }
+    if (a.score.slopes) a.row_pos = scoring->row_pos;  // (nothing else asks for positions)
+  }
+  const size_t need = cache_attention_bytes(p, cu_capacity);
+  if (workspace_bytes < need) return fail(FLOWMM_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  a.q = q; a.out = out;
+  a.part = reinterpret_cast<float *>(workspace);
+  a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.Hq / a.Hkv;
+  a.NB = (int)quant_blocks(p, cu_capacity);
+  a.batch = p->batch;
+  a.SB = 0;
+  if (a.row_pos)
+    for (int b = 0; b < p->batch; ++b) a.SB += p->budget_tokens[b];
+  CacheAttnCall c{cu_capacity, lengths, p->budget_tokens, q_pos, p->n_layers, p->head_dim, rows, p->dtype == FLOWMM_BF16};
+  const hipError_t e = launch_cache_attention(a, c, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "cache attention kernels");
+  return FLOWMM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+FLOWMM_API flowmm_status flowmm_cache_sizes(const flowmm_params *p, const int32_t *cu_capacity, size_t *codes_bytes, size_t *scales_bytes,
+                                 size_t *workspace_bytes) {
+  const flowmm_status st = check_cache(p, cu_capacity, nullptr);
+  if (st != FLOWMM_OK) return st;
+  const size_t units = (size_t)p->n_layers * p->n_kv_heads;
+  if (codes_bytes) *codes_bytes = units * cu_capacity[p->batch] * p->head_dim;
+  if (scales_bytes) *scales_bytes = units * quant_blocks(p, cu_capacity) * 4;
+  if (workspace_bytes) *workspace_bytes = cache_attention_bytes(p, cu_capacity);
+  return FLOWMM_OK;
+}
+
+FLOWMM_API flowmm_status flowmm_cache_quantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                    const int32_t *cu_rows, const void *K_rows, const void *V_rows,
+                                    const flowmm_quantized_cache *cache, void *stream) {
+  return quantize_call(p, cu_capacity, lengths, cu_rows, K_rows, V_rows, cache, false, stream);
+}
+
+FLOWMM_API flowmm_status flowmm_cache_dequantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                      const int32_t *cu_rows, const flowmm_quantized_cache *cache, void *K_rows,
+                                      void *V_rows, void *stream) {
+  return quantize_call(p, cu_capacity, lengths, cu_rows, K_rows, V_rows, cache, true, stream);
+}
+
+FLOWMM_API flowmm_status flowmm_cache_append_quantized(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                            const flowmm_quantized_cache *cache, const void *k_new, const void *v_new, void *stream) {
+  flowmm_status st = check_cache(p, cu_capacity, lengths);
+  if (st != FLOWMM_OK) return st;
+  if (!lengths) return fail(FLOWMM_EINVAL, "lengths must not be NULL");
+  for (int b = 0; b < p->batch; ++b) {
+    const int cap = cu_capacity[b + 1] - cu_capacity[b];
+    if (lengths[b] == cap) return fail(FLOWMM_EINVAL, "the cache of sequence %d is full (%d rows): re-merge it before appending", b, cap);
+  }
+  if ((st = check_quantized(p, cache)) != FLOWMM_OK) return st;
+  if (!k_new || !v_new) return fail(FLOWMM_EINVAL, "k_new and v_new must not be NULL");
+  if (misaligned(k_new) || misaligned(v_new)) return fail(FLOWMM_EINVAL, "k_new and v_new must be 16-byte aligned");
+  if (p->n_kv_heads > 32767) return fail(FLOWMM_EUNSUPPORTED, "more than 32767 kv heads");
+  AppendQuantCall c;
+  c.k_codes = cache->k_codes; c.v_codes = cache->v_codes; c.k_scales = cache->k_scales; c.v_scales = cache->v_scales;
+  c.k_new = k_new; c.v_new = v_new;
+  c.cs_layer = cache->stride_layer; c.cs_head = cache->stride_head; c.cs_tok = cache->stride_token;
+  c.cu_capacity = cu_capacity; c.lengths = lengths;
+  c.NB = (int)quant_blocks(p, cu_capacity);
+  c.batch = p->batch; c.n_layers = p->n_layers; c.Hkv = p->n_kv_heads; c.d = p->head_dim; c.bf16 = p->dtype == FLOWMM_BF16;
+  const hipError_t e = launch_cache_append_quantized(c, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "cache append kernel");
+  return FLOWMM_OK;
+}
+
+FLOWMM_API flowmm_status flowmm_cache_attention(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                     const flowmm_scoring *scoring, const void *q, const void *K_c, const void *V_c,
+                                     void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  flowmm_status st = check_cache(p, cu_capacity, lengths);
+  if (st != FLOWMM_OK) return st;
+  if (!lengths) return fail(FLOWMM_EINVAL, "lengths must not be NULL");
+  if ((st = check_k_strides(p)) != FLOWMM_OK) return st;
+  if (!K_c || !V_c) return fail(FLOWMM_EINVAL, "K_c and V_c must not be NULL");
+  if (misaligned(K_c) || misaligned(V_c)) return fail(FLOWMM_EINVAL, "K_c and V_c must be 16-byte aligned");
+  const int epc = p->dtype == FLOWMM_BF16 ? 8 : 4;
+  CacheAttnArgs a;
+  a.K_c = K_c; a.V_c = V_c; a.k_scales = a.v_scales = nullptr;
+  a.ks_layer = p->k_stride_layer / epc; a.ks_head = p->k_stride_head / epc; a.ks_tok = p->k_stride_token / epc;
+  return cache_attention_call(p, cu_capacity, lengths, scoring, q, out, workspace, workspace_bytes, a, p->dtype == FLOWMM_BF16 ? kRowBF16 : kRowF32, stream);
+}
+
+FLOWMM_API flowmm_status flowmm_cache_attention_quantized(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
+                                               const flowmm_scoring *scoring, const void *q,
+                                               const flowmm_quantized_cache *cache, void *out, void *workspace,
+                                               size_t workspace_bytes, void *stream) {
+  flowmm_status st = check_cache(p, cu_capacity, lengths);
+  if (st != FLOWMM_OK) return st;
+  if (!lengths) return fail(FLOWMM_EINVAL, "lengths must not be NULL");
+  if ((st = check_quantized(p, cache)) != FLOWMM_OK) return st;
+  CacheAttnArgs a;
+  a.K_c = cache->k_codes; a.V_c = cache->v_codes; a.k_scales = cache->k_scales; a.v_scales = cache->v_scales;
+  a.ks_layer = cache->stride_layer / 16; a.ks_head = cache->stride_head / 16; a.ks_tok = cache->stride_token / 16;
+  return cache_attention_call(p, cu_capacity, lengths, scoring, q, out, workspace, workspace_bytes, a, kRowFp8, stream);
+}
+
+FLOWMM_API flowmm_status flowmm_prompt_attention(const flowmm_params *p, const flowmm_scoring *scoring, const void *K, const void *V,
+                                      const void *Q_full, int64_t qf_stride_layer, int64_t qf_stride_head, int64_t qf_stride_token,
+                                      void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  Layout lo;
+  flowmm_status st = build_layout(p, lo, workspace_bytes);
+  if (st != FLOWMM_OK) return st;
+  const Shape &sh = lo.sh;
+  if (!K || !V || !Q_full || !out || !workspace) return fail(FLOWMM_EINVAL, "K, V, Q_full, out and workspace must not be NULL");
+  if (misaligned(K) || misaligned(V) || misaligned(Q_full) || misaligned(out) || misaligned(workspace))
+    return fail(FLOWMM_EINVAL, "K, V, Q_full, out and workspace must be 16-byte aligned");
+  const int es = sh.bf16 ? 2 : 4, epc = 16 / es;
+  const int64_t strides[3] = {qf_stride_layer, qf_stride_head, qf_stride_token};
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < 0 || strides[i] % epc != 0) return fail(FLOWMM_EINVAL, "strides must be non-negative multiples of 16 bytes (%d elements)", epc);
+  if (qf_stride_token < sh.d) return fail(FLOWMM_EINVAL, "token strides must be at least head_dim");
+  // a wave's query rows are addressed with 32-bit byte offsets from its first one
+  if ((31 * qf_stride_token + sh.d) * es >= (int64_t)1 << 32) return fail(FLOWMM_EUNSUPPORTED, "32 query rows span 4 GiB or more");
+  PromptArgs a;
+  if ((st = check_scoring(scoring, scale_of(p), a.score)) != FLOWMM_OK) return st;
+  const int32_t *prefix = scoring ? scoring->prefix : nullptr;
+  if (prefix)
+    for (int b = 0; b < sh.batch; ++b)
+      if (prefix[b] < 0 || prefix[b] > p->cu_seqlens[b + 1] - p->cu_seqlens[b])
+        return fail(FLOWMM_EINVAL, "prefix[%d] = %d is outside [0, length=%d]", b, prefix[b], p->cu_seqlens[b + 1] - p->cu_seqlens[b]);
+  const size_t qo = ((size_t)(sh.n_layers - 1) * qf_stride_layer + (size_t)(sh.Hq - 1) * qf_stride_head + (size_t)(sh.T - 1) * qf_stride_token + sh.d) * es;
+  if (overlaps(out, qo, Q_full, qo) || overlaps(out, qo, K, lo.kv_extent_bytes) || overlaps(out, qo, V, lo.kv_extent_bytes))
+    return fail(FLOWMM_EINVAL, "out must not overlap Q_full, K or V");
+  if (workspace_bytes < lo.workspace_bytes)
+    return fail(FLOWMM_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, lo.workspace_bytes);
+  a.K = K; a.V = V; a.Q = Q_full; a.out = out;
+  a.ks_layer = sh.ks_layer; a.ks_head = sh.ks_head; a.ks_tok = sh.ks_tok;
+  a.qs_layer = qf_stride_layer / epc; a.qs_head = qf_stride_head / epc; a.qs_tok = qf_stride_token / epc;
+  a.n_layers = sh.n_layers; a.Hq = sh.Hq; a.Hkv = sh.Hkv; a.G = sh.G; a.bf16 = sh.bf16; a.d = sh.d;
+  a.image_spans = scoring && scoring->image_spans ? 1 : 0;
+  long long items = 0;
+  for (int b = 0; b < sh.batch; ++b) items += (long long)key_tiles(p, b, kPromptRows) * sh.G;
+  const long long waves = items * sh.n_layers * sh.Hkv;
+  a.ksplit = waves >= 8 * 256 ? 1 : waves >= 4 * 256 ? 2 : 4;
+  std::vector<int32_t> words((size_t)PW_HEADER + (size_t)sh.batch * PS_WORDS, 0);
+  words[PW_BATCH] = sh.batch;
+  words[PW_SPANS] = (int32_t)words.size();
+  int wgs = 0;
+  for (int b = 0; b < sh.batch; ++b) {
+    int32_t *r = &words[PW_HEADER + (size_t)b * PS_WORDS];
+    r[PS_WG] = wgs; r[PS_TOK] = p->cu_seqlens[b]; r[PS_L] = p->cu_seqlens[b + 1] - p->cu_seqlens[b];
+    r[PS_PREFIX] = prefix ? prefix[b] : 0;
+    r[PS_SPAN] = p->cu_spans[b]; r[PS_N_SPANS] = p->cu_spans[b + 1] - p->cu_spans[b];
+    const long long n = (long long)key_tiles(p, b, kPromptRows) * sh.G, per = kPromptWaves / a.ksplit;
+    wgs += (int)((n + per - 1) / per);
+  }
+  a.wgs_total = wgs;
+  if (a.image_spans)
+    for (int j = 0; j < sh.n_spans; ++j) { words.push_back(p->spans[j].end); words.push_back(p->spans[j].modality == FLOWMM_IMAGE); }
+  a.meta = reinterpret_cast<const int *>(reinterpret_cast<char *>(workspace) + lo.rg.meta);
+  const int n_words = words.size() <= kMetaArgWords ? (int)words.size() : 0;
+  hipError_t e;
+  if (n_words == 0) {  // (fewer than the metadata words that the workspace has room for)
+    Ctx c;
+    std::memset(&c, 0, sizeof(c));
+    c.stream = reinterpret_cast<hipStream_t>(stream);
+    c.meta = reinterpret_cast<int *>(reinterpret_cast<char *>(workspace) + lo.rg.meta);
+    if ((e = launch_meta_upload(c, words.data(), (int)words.size(), false)) != hipSuccess) return hip_fail(e, "metadata upload");
+  }
+  if ((e = launch_prompt_attention(a, words.data(), n_words, reinterpret_cast<hipStream_t>(stream))) != hipSuccess) return hip_fail(e, "prompt attention kernel");
+  return FLOWMM_OK;
+}
+
+}  // extern "C"

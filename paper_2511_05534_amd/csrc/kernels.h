@@ -171,6 +171,99 @@ struct InPlaceArgs {
 bool merge_in_place_fits(const Shape &sh);
 hipError_t launch_merge_in_place(const Ctx &c, void *K_c, void *V_c);  // after launch_merge_csr
 
+// the cache in 8 bits (cache_quantize.hip): rows of the batch's sequences to codes and back.  Row strides in 16-byte chunks, code strides in bytes
+constexpr int kQuantRows = 32;  // of a block, which shares a scale
+constexpr int kQuantSeqs = 64;  // sequences per launch
+struct QuantArgs {
+  const void *K_rows, *V_rows;   // written by the way back
+  void *k_codes, *v_codes;
+  float *k_scales, *v_scales;    // [Lyr][Hkv][NB]
+  long long ks_layer, ks_head, ks_tok, cs_layer, cs_head, cs_tok;
+  int Hkv, NB, n_seqs, blocks;   // blocks: valid ones of this launch's sequences
+  struct Seq { int first, len, row, code_row, block; } seq[kQuantSeqs];  // first of those blocks, valid rows, first row, first code row, first scale
+};
+struct QuantCall {
+  const int *cu_capacity, *lengths, *cu_rows;
+  int batch, n_layers, d;
+  bool bf16, back;
+};
+hipError_t launch_cache_quantize(QuantArgs a, const QuantCall &c, hipStream_t stream);
+
+// one token's rows to codes; N as for AppendArgs
+template <int N>
+struct AppendQuantArgs {
+  void *k_codes, *v_codes;
+  float *k_scales, *v_scales;
+  const void *k_new, *v_new;     // [Lyr][Hkv][batch][d] contiguous, from the first sequence of this launch on
+  long long cs_layer, cs_head, cs_tok;
+  int NB, batch;
+  int row[N];                    // code row that the i-th sequence of the launch appends to
+  unsigned where[N];             // its scale's number and, in the low five bits, its row inside the block
+};
+struct AppendQuantCall {
+  void *k_codes, *v_codes;
+  float *k_scales, *v_scales;
+  const void *k_new, *v_new;
+  long long cs_layer, cs_head, cs_tok;
+  const int *cu_capacity, *lengths;
+  int NB, batch, n_layers, Hkv, d;
+  bool bf16;
+};
+hipError_t launch_cache_append_quantized(const AppendQuantCall &c, hipStream_t stream);
+
+// how an attention makes scores of products of q and k, in the log2 domain (attention_core.h)
+struct ScoreArgs {
+  float cl;            // scale * log2(e)
+  float cap, cap_in;   // cap * log2(e), or 0: not capped; scale / cap
+  const float *slopes; // [Hq] or NULL
+};
+
+// one step of attention over a cache with head room (cache_attention.hip)
+constexpr int kCacheAttnSeqs = 64;        // sequences per launch
+constexpr int kCacheAttnLeastPart = 128;  // rows of a part (workgroup) at the least, where a sequence is cut
+constexpr int kCacheAttnMostParts = 64;   // parts of a sequence
+constexpr int kCacheAttnTasks = 1024;     // workgroups that sequences are cut for: at most this many over the (layer, kv head) units and one a sequence
+enum RowKind { kRowF32, kRowBF16, kRowFp8 };
+struct CacheAttnArgs {
+  const void *q;                // [Lyr][Hq][batch][d]
+  const void *K_c, *V_c;        // rows or codes
+  const float *k_scales, *v_scales;
+  void *out;
+  float *part;                  // [Lyr][Hq][tasks][d + 2] weighted V, max, sum of the sequences of several tasks
+  long long ks_layer, ks_head, ks_tok;  // 16-byte chunks
+  const int *row_pos;           // [Lyr][Hkv][SB] or NULL
+  ScoreArgs score;
+  int Hq, Hkv, G, NB, SB, batch;
+  int chunk;                    // rows of a task
+  int b0, n_seqs, tasks, g0;    // sequences b0 .. b0 + n_seqs - 1 are in this launch, cut into tasks; first query head inside its kv group
+  struct Seq { int task, len, row, block, merged, slot, q_pos, pad; };
+  alignas(64) Seq seq[kCacheAttnSeqs + 1];
+};
+struct CacheAttnCall {
+  const int *cu_capacity, *lengths, *budgets, *q_pos;
+  int n_layers, d;
+  RowKind rows;
+  bool bf16;                    // q and out
+};
+hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnCall &c, hipStream_t stream);
+
+// the prompt's attention (prompt_attention.hip); its sequences and spans travel as metadata words of its own
+enum PromptWord { PW_BATCH = 0, PW_SPANS /* word offset of the spans' ends and modalities */, PW_HEADER };
+enum PromptSeqWord { PS_WG = 0 /* first workgroup of a (kv head, layer) */, PS_TOK, PS_L, PS_PREFIX, PS_SPAN, PS_N_SPANS, PS_WORDS };
+constexpr int kPromptWaves = 8, kPromptRows = 32;  // query rows of a wave
+struct PromptArgs {
+  const void *K, *V, *Q;
+  void *out;
+  const int *meta;              // the words' place in the workspace
+  long long ks_layer, ks_head, ks_tok, qs_layer, qs_head, qs_tok;  // 16-byte chunks
+  ScoreArgs score;
+  int n_layers, Hq, Hkv, G, bf16, d;
+  int wgs_total, group;         // workgroups per (kv head, layer); units that the grid takes in turn
+  int ksplit;                   // waves that share the query rows and split the keys
+  int image_spans;
+};
+hipError_t launch_prompt_attention(const PromptArgs &a, const int *words, int n_words, hipStream_t stream);
+
 constexpr int kMetaChunkWords = 960;
 struct MetaChunk { int w[kMetaChunkWords]; };
 

@@ -15,7 +15,9 @@ const char *const kNames[KID_COUNT] = {"meta_upload", "expand_modality", "score_
                                        "score_colsum", "select", "match", "merge_csr", "merge_tasks",
                                        "unit_plan", "unit_match", "unit_merge", "unit_flow_merge",
                                        "flow_exact", "decode_partial", "decode_combine", "cache_append",
-                                       "cache_store_rows", "merge_in_place", "score_resident", "select_match"};
+                                       "cache_store_rows", "merge_in_place", "score_resident", "select_match",
+                                       "cache_quantize", "cache_dequantize", "cache_append_quantized", "cache_attention", "cache_attention_combine",
+                                       "prompt_attention"};
 
 struct Record { int id; hipEvent_t start, stop; };
 

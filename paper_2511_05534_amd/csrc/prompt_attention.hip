@@ -1,0 +1,336 @@
+// The prompt's attention: every token of every packed sequence as a query over the keys that it sees,
+//   o_t = softmax_j(score(q_t k_j)) v_j,   j <= reach(t),
+// reach(t) = t, or the last token of the prefix or of the image span that t lies in: one number per row, which never falls from row to
+// row, is the whole mask.  The attention matrix is never stored: one pass over the keys with the running maximum and sum of each row.
+//
+// A wave holds 32 query rows of one head in registers, as the second operand: the accumulators of S = K Q^T hold keys in their registers and
+// rows in their lanes, so that a row's statistics are a lane's own and P is, register for register, an operand of O^T = V^T P^T.  The eight
+// waves of a workgroup take the heads of the kv group at the same rows first and walk over one stream of K and V tiles, which direct
+// global->LDS loads fill, double buffered.  V comes out of LDS transposed (ds_read_b64_tr_b16; fp32: by ordinary reads).
+// Where rows are few, two or four waves share them and split the keys.
+//
+// bf16: P is rounded to bf16 for the second product, as V is one (relative 2^-9 a weight, each its own, so that it stays below the
+// rounding of the result wherever many keys count); its sum is of the fp32 weights.  fp32: both products by the fp32 matrix instructions.
+#include <cfloat>
+
+#include "attention_core.h"
+#include "decode_core.h"
+#include "kernels.h"
+#include "profile.h"
+
+namespace flowmm {
+
+namespace {
+
+constexpr int kPThreads = kPromptWaves * 64;
+constexpr int kPromptGroupWgs = 4096;  // workgroups of a group of units
+
+// V rows in LDS: whole rows by direct loads as in KeyTile, the chunks of a row permuted so that the four rows that 16 lanes transpose, 32 bytes
+// of each, lie in different banks
+template <bool BF16, int D, int ROWS>
+struct ValueTile {
+  static constexpr int NCH = Cfg<BF16, D>::NCH, kChunks = ROWS * NCH, RPI = 64 / NCH;
+  __device__ static __forceinline__ int permute(int r) { return BF16 ? (NCH == 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) : ((r >> 2) & 1) << 3; }
+  __device__ static __forceinline__ int slot(int r, int ch) { return r * NCH + (ch ^ permute(r)); }
+  template <int WAVES>
+  __device__ static __forceinline__ void request(const uint4 *src, long long row_stride, int r0, int last, uint4 *tile, int wave) {
+    const int lane = lane_id_here(), j = lane / NCH;
+    constexpr int kLoads = kChunks / 64;
+    static_assert(kLoads % WAVES == 0, "every wave asks for as many rows");
+    const uint4 *base = src + r0 * row_stride;
+    const bool near = row_stride < (1ll << 32) / (16 * ROWS);
+#pragma unroll
+    for (int i = 0; i < kLoads / WAVES; ++i) {
+      const int g = i * WAVES + wave, rt = g * RPI + j, r = min(rt, last - r0), ch = (lane % NCH) ^ permute(rt);
+      if (near) load_to_lds<16>(base, ((unsigned)r * (unsigned)row_stride + (unsigned)ch) * 16u, tile + g * 64);
+      else tile[g * 64 + lane] = base[r * row_stride + ch];
+    }
+  }
+};
+
+// the last key that row q of the sequence sees
+__device__ __forceinline__ int reach_of(const PromptArgs &a, ScalarInts meta, const int L, const int prefix, const int span0, const int n_spans, int q) {
+  int r = q < prefix ? prefix - 1 : q;
+  if (a.image_spans) {
+    // the span of q: the first whose end is behind it
+    const ScalarInts spans = meta + meta[PW_SPANS] + 2 * span0;
+    int lo = 0, hi = n_spans - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (spans[2 * mid] > q) hi = mid; else lo = mid + 1;
+    }
+    if (spans[2 * lo + 1]) r = max(r, spans[2 * lo] - 1);
+  }
+  return min(r, L - 1);
+}
+
+template <bool BF16, int D, int KS, bool SCORED>
+__global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelArgs<PromptArgs> k) {
+  const PromptArgs &a = k.a;
+  using CF = Cfg<BF16, D>;
+  using TL = KeyTile<BF16, D>;
+  constexpr int NCH = CF::NCH, NF = CF::NF, KT = TL::kRows, CT = D / 32;
+  using VT = ValueTile<BF16, D, KT>;
+  constexpr int kBuffer = TL::kChunks + VT::kChunks;
+  constexpr float kLazy = 8.f;  // the running maximum follows once it is 2^8 behind: exact all the same, z stays far below overflow
+  extern __shared__ __align__(16) uint4 lds_kv[];  // [2] K tile, V tile; at the end the waves' outputs
+
+  const ScalarInts meta = first_meta(k, a.meta);
+  // groups of units, a group's units in turn, late positions (long key streams) first
+  const int units = a.n_layers * a.Hkv, u0 = blockIdx.x / (a.group * a.wgs_total) * a.group, n_group = min(a.group, units - u0);
+  const int rest = blockIdx.x - u0 * a.wgs_total, turn = rest / n_group, unit = u0 + rest - turn * n_group, x = a.wgs_total - 1 - turn;
+  const int l = unit / a.Hkv, gkv = unit - l * a.Hkv;
+  int b = 0;
+  for (int lo = 0, hi = meta[PW_BATCH]; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (meta[PW_HEADER + mid * PS_WORDS + PS_WG] <= x) b = lo = mid; else hi = mid;
+  }
+  const ScalarInts rec = meta + PW_HEADER + b * PS_WORDS;
+  const int L = rec[PS_L], tok = rec[PS_TOK], prefix = rec[PS_PREFIX], span0 = rec[PS_SPAN], n_spans = rec[PS_N_SPANS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+  // item i of the sequence: head i % G of the kv group, query rows [32 * (i / G), + 32)
+  const int items = (L + kPromptRows - 1) / kPromptRows * a.G;
+  constexpr int kItems = kPromptWaves / KS;
+  const int ks = wave / kItems;  // this wave takes every KS-th block of 32 keys, from block ks on
+  const int first = (x - rec[PS_WG]) * kItems, mine = first + wave - ks * kItems, item = min(mine, items - 1);
+  const bool active = mine < items;
+  const int pb = item / a.G, h = gkv * a.G + (item - pb * a.G), p0 = pb * kPromptRows;
+  const int wg_row = min((min(first + kItems, items) - 1) / a.G * kPromptRows + kPromptRows, L) - 1;  // last row of the workgroup
+  const int wg_last = __builtin_amdgcn_readfirstlane(reach_of(a, meta, L, prefix, span0, n_spans, wg_row));
+  const int limit = reach_of(a, meta, L, prefix, span0, n_spans, min(p0 + n, L - 1));  // of this lane's row
+  const int w_first = __builtin_amdgcn_readfirstlane(limit), w_last = active ? __builtin_amdgcn_readlane(limit, 31) : -1;
+
+  // ---- this wave's query rows (clamped past the end of the sequence), through its share of the LDS ----
+  uint4 qf[NF];
+  const uint4 *Q = reinterpret_cast<const uint4 *>(a.Q) + (long long)l * a.qs_layer + (long long)h * a.qs_head + (long long)(tok + p0) * a.qs_tok;
+  static_assert(kPromptWaves * 32 * NCH <= 2 * kBuffer, "the waves' query rows");
+  fetch_rows_staged<BF16, D>(Q, (unsigned)a.qs_tok, min(p0 + n, L - 1) - p0, lds_kv + wave * 32 * NCH, qf);
+  __syncthreads();  // the tiles may overwrite the other waves' shares now
+
+  const long long kv_at = (long long)l * a.ks_layer + (long long)gkv * a.ks_head + (long long)tok * a.ks_tok;
+  const uint4 *K = reinterpret_cast<const uint4 *>(a.K) + kv_at, *V = reinterpret_cast<const uint4 *>(a.V) + kv_at;
+  const float cl = a.score.cl;
+  const float slope = SCORED && a.score.slopes ? a.score.slopes[h] * 1.4426950408889634f : 0.f;
+  float m = -FLT_MAX, z = 0.f;  // of row n; z over the keys of this half-wave
+  f32x16_t o[CT];               // [channel 32 c + ..][row n]
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+
+  const int ntiles = wg_last / KT + 1;
+  auto request = [&](int t) {
+    uint4 *to = lds_kv + (t & 1) * kBuffer;
+    TL::template request<kPromptWaves>(K, a.ks_tok, t * KT, L - 1, to, wave);
+    VT::template request<kPromptWaves>(V, a.ks_tok, t * KT, L - 1, to + TL::kChunks, wave);
+  };
+  request(0);
+  for (int t = 0; t < ntiles; ++t) {
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's part of tile t has landed
+    __syncthreads();                // ... and everybody else's; tile t-1 is no longer read
+    if (t + 1 < ntiles) request(t + 1);
+    const char *tile = reinterpret_cast<const char *>(lds_kv + (t & 1) * kBuffer);
+    const char *rows0 = tile + TL::frag_offset(n, half, 0), *rows1 = tile + TL::frag_offset(n, half, 1);
+    const uint4 *values = lds_kv + (t & 1) * kBuffer + TL::kChunks;
+#pragma unroll 1
+    for (int kb = ks; kb < KT / 32; kb += KS) {
+      const int key0 = t * KT + 32 * kb;
+      if (key0 > w_last) break;  // nothing of this wave may see these keys
+      f32x16_t s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      const char *blk0 = rows0 + kb * TL::block_bytes(1), *blk1 = rows1 + kb * TL::block_bytes(1);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        const uint4 kf = *reinterpret_cast<const uint4 *>((f & 1 ? blk1 : blk0) + 64 * (f >> 1));
+        mma_chunk<BF16>(s, kf, qf[f]);  // [key][row]
+      }
+      const bool masked = key0 + 31 > w_first;
+      // ---- scores ----
+      if constexpr (SCORED) {
+        if (a.score.cap > 0.f) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = capped<!BF16>(a.score, s[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] *= cl;
+        }
+        if (a.score.slopes) {
+          const int ahead = key0 + 4 * half - (p0 + n);  // of key 0 of this lane
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = fmaf(-slope, fabsf((float)(ahead + acc_row(i, 0))), s[i]);
+        }
+      } else {
+        // (rounded here, not by a fused multiply-add with the maximum below: what that leaves of a product's rounding is 2^-24 of it, and logits may be 1e30)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] *= cl;
+      }
+      if (masked) {
+        const int last = limit - key0 - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = acc_row(i, 0) <= last ? s[i] : -INFINITY;
+      }
+      float tm = fmaxf(s[0], s[1]);
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) tm = fmaxf(fmaxf(tm, s[i]), s[i + 1]);
+      if (__any(tm > m + kLazy)) {
+        const float M = fmaxf(m, fmaxf(tm, __shfl_xor(tm, 32, 64))), f = fast_exp2(m - M);
+        z *= f;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[c][i] *= f;
+        m = M;
+      }
+      float za = 0.f, zb = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        s[i] = fast_exp2(s[i] - m);
+        s[i + 1] = fast_exp2(s[i + 1] - m);
+        za += s[i];
+        zb += s[i + 1];
+      }
+      z += za + zb;
+      // ---- O += V^T P; a masked block's infinite or undefined values may only reach the rows that see them: taken out here, added below ----
+      bool odd = false;
+      if constexpr (BF16) {
+        uint4 pf[2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+          pf[kk] = make_uint4(pack_bf16(s[8 * kk], s[8 * kk + 1]), pack_bf16(s[8 * kk + 2], s[8 * kk + 3]), pack_bf16(s[8 * kk + 4], s[8 * kk + 5]), pack_bf16(s[8 * kk + 6], s[8 * kk + 7]));
+        const int i16 = lane & 15, g16 = (lane >> 4) & 1;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            uint4 vf;
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+              const int r = 32 * kb + 16 * kk + 8 * jj + 4 * half + (i16 >> 2);
+              const char *from = reinterpret_cast<const char *>(values + VT::slot(r, 4 * c + 2 * g16 + ((i16 & 3) >> 1))) + 8 * (i16 & 1);
+              const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+              __builtin_memcpy(reinterpret_cast<char *>(&vf) + 8 * jj, &v, 8);
+            }
+            if (masked) {
+              unsigned *w = reinterpret_cast<unsigned *>(&vf);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const bool hi = (w[e] & 0x7f800000u) == 0x7f800000u, lo = (w[e] & 0x7f80u) == 0x7f80u;
+                odd |= hi | lo;
+                w[e] = (hi ? 0u : w[e] & 0xffff0000u) | (lo ? 0u : w[e] & 0xffffu);
+              }
+            }
+            mma_chunk<true>(o[c], vf, pf[kk]);
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            float v = reinterpret_cast<const float *>(values + VT::slot(32 * kb + acc_row(i, half), 8 * c + (n >> 2)))[n & 3];
+            if (masked) {
+              const bool bad = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+              odd |= bad;
+              v = bad ? 0.f : v;
+            }
+            o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], o[c], 0, 0, 0);
+          }
+      }
+      if (masked && __any(odd)) {
+#pragma unroll 1
+        for (int j = 0; j < 32; ++j) {
+          if (key0 + j >= L) break;
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int ch = 32 * c + acc_row(i, half);
+              float v;
+              if constexpr (BF16) v = bf16_bits_to_float(reinterpret_cast<const uint16_t *>(values + VT::slot(32 * kb + j, ch >> 3))[ch & 7]);
+              else v = reinterpret_cast<const float *>(values + VT::slot(32 * kb + j, ch >> 2))[ch & 3];
+              if (!(fabsf(v) < INFINITY) && key0 + j <= limit) o[c][i] += v;
+            }
+        }
+      }
+    }
+  }
+
+  // ---- fold the half-waves, then the waves with the same rows; out through LDS, whole rows ----
+  z += __shfl_xor(z, 32, 64);
+  __syncthreads();  // nobody reads tiles any more
+  constexpr int SS = D + 4;  // row of a wave's output in LDS: D channels, m, z
+  float *st = reinterpret_cast<float *>(lds_kv) + wave * 32 * SS;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<float4 *>(st + n * SS + 32 * c + acc_row(i, half)) = make_float4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
+  if (half == 0) { st[n * SS + D] = m; st[n * SS + D + 1] = z; }
+  __syncthreads();
+  if (!active) return;
+  // the KS waves of the rows store a share of them each
+  constexpr int EPC = CF::kElemsPerChunk, RPT = 64 / NCH;
+  uint4 *out = reinterpret_cast<uint4 *>(a.out) + (long long)l * a.qs_layer + (long long)h * a.qs_head + (long long)(tok + p0) * a.qs_tok;
+  const float *st0 = reinterpret_cast<const float *>(lds_kv) + (wave - ks * kItems) * 32 * SS;
+#pragma unroll 1
+  for (int r = ks * (32 / KS) + lane / NCH; r < (ks + 1) * (32 / KS); r += RPT) {
+    if (p0 + r >= L) break;
+    float M = -FLT_MAX, zz = 0.f, f[EPC];
+#pragma unroll
+    for (int w = 0; w < KS; ++w) M = fmaxf(M, st0[(w * kItems * 32 + r) * SS + D]);
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) f[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < KS; ++w) {
+      const float *row = st0 + (w * kItems * 32 + r) * SS;
+      const float g = fast_exp2(row[D] - M);
+      zz = fmaf(row[D + 1], g, zz);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) f[e] = fmaf(row[lane % NCH * EPC + e], g, f[e]);
+    }
+    const float inv = 1.f / zz;
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) f[e] *= inv;
+    out[r * a.qs_tok + lane % NCH] = floats_to_chunk<BF16>(f);
+  }
+}
+
+template <bool BF16, int D, int KS, bool SCORED>
+hipError_t launch_prompt_t(const KernelArgs<PromptArgs> &k, unsigned grid, hipStream_t stream) {
+  const size_t tiles = 2 * (size_t)(KeyTile<BF16, D>::kChunks + ValueTile<BF16, D, KeyTile<BF16, D>::kRows>::kChunks) * 16;
+  const size_t outputs = (size_t)kPromptWaves * 32 * (D + 4) * sizeof(float);
+  const size_t lds = tiles > outputs ? tiles : outputs;
+  const hipError_t e = allow_full_lds<prompt_attention_kernel<BF16, D, KS, SCORED>>();
+  if (e != hipSuccess) return e;
+  ProfScope ps(stream, KID_PROMPT_ATTENTION);
+  prompt_attention_kernel<BF16, D, KS, SCORED><<<dim3(grid), kPThreads, lds, stream>>>(k);
+  return hipGetLastError();
+}
+
+template <bool BF16, int D>
+hipError_t launch_prompt_d(const KernelArgs<PromptArgs> &k, unsigned grid, hipStream_t stream) {
+  const bool scored = k.a.score.cap > 0.f || k.a.score.slopes;
+  switch (k.a.ksplit) {
+    case 4: return scored ? launch_prompt_t<BF16, D, 4, true>(k, grid, stream) : launch_prompt_t<BF16, D, 4, false>(k, grid, stream);
+    case 2: return scored ? launch_prompt_t<BF16, D, 2, true>(k, grid, stream) : launch_prompt_t<BF16, D, 2, false>(k, grid, stream);
+    default: return scored ? launch_prompt_t<BF16, D, 1, true>(k, grid, stream) : launch_prompt_t<BF16, D, 1, false>(k, grid, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_prompt_attention(const PromptArgs &args, const int *words, int n_words, hipStream_t stream) {
+  PromptArgs a = args;
+  const int units = a.n_layers * a.Hkv;
+  const long long grid = (long long)units * a.wgs_total;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  a.group = (kPromptGroupWgs / a.wgs_total + 7) / 8 * 8;
+  if (a.group < 8) a.group = 8;
+  if (a.group > units) a.group = units;
+  KernelArgs<PromptArgs> k;
+  fill_kernel_args(k, a, words, n_words);
+  if (a.bf16) return a.d == 128 ? launch_prompt_d<true, 128>(k, (unsigned)grid, stream) : launch_prompt_d<true, 64>(k, (unsigned)grid, stream);
+  return a.d == 128 ? launch_prompt_d<false, 128>(k, (unsigned)grid, stream) : launch_prompt_d<false, 64>(k, (unsigned)grid, stream);
+}
+
+}  // namespace flowmm

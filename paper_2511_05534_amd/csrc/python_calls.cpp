@@ -195,9 +195,56 @@ PyObject *cache_remerge(PyObject *, Args a, Py_ssize_t n) {
   return call([&] { return flowmm_cache_remerge(p, cu.data(), len.data(), seq, K, V, Q, &b, ws, bytes, stream); });
 }
 
+// (params, cu_capacity, lengths, cache, k_new, v_new, stream)
+PyObject *cache_append_quantized(PyObject *, Args a, Py_ssize_t n) {
+  const flowmm_params *p; Ints cu, len; const flowmm_quantized_cache *c; const void *k, *v; void *stream;
+  if (!count(n, 7) || !as_pointer(a[0], &p) || !cu.take(a[1], sequences(p) + 1, "cu_capacity") || !len.take(a[2], sequences(p), "lengths") ||
+      !as_pointer(a[3], &c) || !as_pointer(a[4], &k) || !as_pointer(a[5], &v) || !as_pointer(a[6], &stream)) return nullptr;
+  return call([&] { return flowmm_cache_append_quantized(p, cu.data(), len.data(), c, k, v, stream); });
+}
+
+// (params, cu_capacity, lengths, cu_rows, K_rows, V_rows, cache, back, stream)
+PyObject *cache_quantize(PyObject *, Args a, Py_ssize_t n) {
+  const flowmm_params *p; Ints cu, len, at; const flowmm_quantized_cache *c; void *K, *V, *stream; int32_t back;
+  if (!count(n, 9) || !as_pointer(a[0], &p) || !cu.take(a[1], sequences(p) + 1, "cu_capacity") || !len.take(a[2], sequences(p), "lengths") ||
+      !at.take(a[3], sequences(p), "cu_rows") || !as_pointer(a[4], &K) || !as_pointer(a[5], &V) || !as_pointer(a[6], &c) || !as_int32(a[7], &back) ||
+      !as_pointer(a[8], &stream)) return nullptr;
+  return call([&] {
+    return back ? flowmm_cache_dequantize(p, cu.data(), len.data(), at.data(), c, K, V, stream) : flowmm_cache_quantize(p, cu.data(), len.data(), at.data(), K, V, c, stream);
+  });
+}
+
+// (params, cu_capacity, lengths, scoring, q, K_c, V_c, out, workspace, workspace_bytes, stream)
+PyObject *cache_attention(PyObject *, Args a, Py_ssize_t n) {
+  const flowmm_params *p; Ints cu, len; const flowmm_scoring *sc; const void *q, *K, *V; void *out, *ws, *stream; size_t bytes;
+  if (!count(n, 11) || !as_pointer(a[0], &p) || !cu.take(a[1], sequences(p) + 1, "cu_capacity") || !len.take(a[2], sequences(p), "lengths") ||
+      !as_pointer(a[3], &sc) || !as_pointer(a[4], &q) || !as_pointer(a[5], &K) || !as_pointer(a[6], &V) || !as_pointer(a[7], &out) ||
+      !as_pointer(a[8], &ws) || !as_size(a[9], &bytes) || !as_pointer(a[10], &stream)) return nullptr;
+  return call([&] { return flowmm_cache_attention(p, cu.data(), len.data(), sc, q, K, V, out, ws, bytes, stream); });
+}
+
+// (params, cu_capacity, lengths, scoring, q, cache, out, workspace, workspace_bytes, stream)
+PyObject *cache_attention_quantized(PyObject *, Args a, Py_ssize_t n) {
+  const flowmm_params *p; Ints cu, len; const flowmm_scoring *sc; const flowmm_quantized_cache *c; const void *q; void *out, *ws, *stream; size_t bytes;
+  if (!count(n, 10) || !as_pointer(a[0], &p) || !cu.take(a[1], sequences(p) + 1, "cu_capacity") || !len.take(a[2], sequences(p), "lengths") ||
+      !as_pointer(a[3], &sc) || !as_pointer(a[4], &q) || !as_pointer(a[5], &c) || !as_pointer(a[6], &out) || !as_pointer(a[7], &ws) ||
+      !as_size(a[8], &bytes) || !as_pointer(a[9], &stream)) return nullptr;
+  return call([&] { return flowmm_cache_attention_quantized(p, cu.data(), len.data(), sc, q, c, out, ws, bytes, stream); });
+}
+
+// (params, scoring, K, V, Q_full, strides of it (3), out, workspace, workspace_bytes, stream)
+PyObject *prompt_attention(PyObject *, Args a, Py_ssize_t n) {
+  const flowmm_params *p; const flowmm_scoring *sc; const void *K, *V, *Q; void *out, *ws, *stream; size_t bytes; long long st[3];
+  if (!count(n, 12) || !as_pointer(a[0], &p) || !as_pointer(a[1], &sc) || !as_pointer(a[2], &K) || !as_pointer(a[3], &V) || !as_pointer(a[4], &Q) ||
+      !as_int64(a[5], &st[0]) || !as_int64(a[6], &st[1]) || !as_int64(a[7], &st[2]) || !as_pointer(a[8], &out) || !as_pointer(a[9], &ws) ||
+      !as_size(a[10], &bytes) || !as_pointer(a[11], &stream)) return nullptr;
+  return call([&] { return flowmm_prompt_attention(p, sc, K, V, Q, st[0], st[1], st[2], out, ws, bytes, stream); });
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(plan), METHOD(merge), METHOD(plan_merge), METHOD(plan_merge_static), METHOD(decode_attention),
-                         METHOD(cache_append), METHOD(cache_remerge), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(cache_append), METHOD(cache_remerge), METHOD(cache_append_quantized), METHOD(cache_quantize), METHOD(cache_attention),
+                         METHOD(cache_attention_quantized), METHOD(prompt_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_flowmm_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
