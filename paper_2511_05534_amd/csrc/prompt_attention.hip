@@ -12,6 +12,7 @@
 // bf16: P is rounded to bf16 for the second product, as V is one (relative 2^-9 a weight, each its own, so that it stays below the
 // rounding of the result wherever many keys count); its sum is of the fp32 weights.  fp32: both products by the fp32 matrix instructions.
 #include <cfloat>
+#include <type_traits>
 
 #include "attention_core.h"
 #include "decode_core.h"
@@ -124,95 +125,105 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
     TL::template request<kPromptWaves>(K, a.ks_tok, t * KT, L - 1, to, wave);
     VT::template request<kPromptWaves>(V, a.ks_tok, t * KT, L - 1, to + TL::kChunks, wave);
   };
-  request(0);
-  for (int t = 0; t < ntiles; ++t) {
-    __builtin_amdgcn_s_waitcnt(0);  // this wave's part of tile t has landed
-    __syncthreads();                // ... and everybody else's; tile t-1 is no longer read
-    if (t + 1 < ntiles) request(t + 1);
+  // blocks kb, kb + KS, .. (NB of them) of tile t; MASKED: some row of the wave does not see all of their keys
+  auto blocks = [&](auto nb, auto masked_t, int t, int kb) __attribute__((always_inline)) {
+    constexpr int NB = decltype(nb)::value;
+    constexpr bool MASKED = decltype(masked_t)::value;
     const char *tile = reinterpret_cast<const char *>(lds_kv + (t & 1) * kBuffer);
     const char *rows0 = tile + TL::frag_offset(n, half, 0), *rows1 = tile + TL::frag_offset(n, half, 1);
     const uint4 *values = lds_kv + (t & 1) * kBuffer + TL::kChunks;
-#pragma unroll 1
-    for (int kb = ks; kb < KT / 32; kb += KS) {
-      const int key0 = t * KT + 32 * kb;
-      if (key0 > w_last) break;  // nothing of this wave may see these keys
-      f32x16_t s;
+    const int key0 = t * KT + 32 * kb;
+    f32x16_t s[NB];  // [key][row]
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-      const char *blk0 = rows0 + kb * TL::block_bytes(1), *blk1 = rows1 + kb * TL::block_bytes(1);
+    for (int u = 0; u < NB; ++u)
 #pragma unroll
-      for (int f = 0; f < NF; ++f) {
-        const uint4 kf = *reinterpret_cast<const uint4 *>((f & 1 ? blk1 : blk0) + 64 * (f >> 1));
-        mma_chunk<BF16>(s, kf, qf[f]);  // [key][row]
+      for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        const uint4 kf = *reinterpret_cast<const uint4 *>((f & 1 ? rows1 : rows0) + (kb + u * KS) * TL::block_bytes(1) + 64 * (f >> 1));
+        mma_chunk<BF16>(s[u], kf, qf[f]);
       }
-      const bool masked = key0 + 31 > w_first;
-      // ---- scores ----
+
+    // ---- scores ----
+#pragma unroll
+    for (int u = 0; u < NB; ++u) {
       if constexpr (SCORED) {
         if (a.score.cap > 0.f) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = capped<!BF16>(a.score, s[i]);
+          for (int i = 0; i < 16; ++i) s[u][i] = capped<!BF16>(a.score, s[u][i]);
         } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] *= cl;
+          for (int i = 0; i < 16; ++i) s[u][i] *= cl;
         }
         if (a.score.slopes) {
-          const int ahead = key0 + 4 * half - (p0 + n);  // of key 0 of this lane
+          const int ahead = key0 + 32 * u * KS + 4 * half - (p0 + n);  // of key 0 of this lane
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = fmaf(-slope, fabsf((float)(ahead + acc_row(i, 0))), s[i]);
+          for (int i = 0; i < 16; ++i) s[u][i] = fmaf(-slope, fabsf((float)(ahead + acc_row(i, 0))), s[u][i]);
         }
       } else {
         // (rounded here, not by a fused multiply-add with the maximum below: what that leaves of a product's rounding is 2^-24 of it, and logits may be 1e30)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] *= cl;
+        for (int i = 0; i < 16; ++i) s[u][i] *= cl;
       }
-      if (masked) {
-        const int last = limit - key0 - 4 * half;
+      if constexpr (MASKED) {
+        const int last = limit - key0 - 32 * u * KS - 4 * half;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = acc_row(i, 0) <= last ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[u][i] = acc_row(i, 0) <= last ? s[u][i] : -INFINITY;
       }
-      float tm = fmaxf(s[0], s[1]);
+    }
+    float tm = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
-      for (int i = 2; i < 16; i += 2) tm = fmaxf(fmaxf(tm, s[i]), s[i + 1]);
-      if (__any(tm > m + kLazy)) {
-        const float M = fmaxf(m, fmaxf(tm, __shfl_xor(tm, 32, 64))), f = fast_exp2(m - M);
-        z *= f;
+    for (int u = 0; u < NB; ++u)
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+      for (int i = u ? 0 : 2; i < 16; i += 2) tm = fmaxf(fmaxf(tm, s[u][i]), s[u][i + 1]);
+    if (__any(tm > m + kLazy)) {
+      const float M = fmaxf(m, fmaxf(tm, __shfl_xor(tm, 32, 64))), f = fast_exp2(m - M);
+      z *= f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[c][i] *= f;
-        m = M;
-      }
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] *= f;
+      m = M;
+    }
+#pragma unroll
+    for (int u = 0; u < NB; ++u) {
       float za = 0.f, zb = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        s[i] = fast_exp2(s[i] - m);
-        s[i + 1] = fast_exp2(s[i + 1] - m);
-        za += s[i];
-        zb += s[i + 1];
+        s[u][i] = fast_exp2(s[u][i] - m);
+        s[u][i + 1] = fast_exp2(s[u][i + 1] - m);
+        za += s[u][i];
+        zb += s[u][i + 1];
       }
       z += za + zb;
-      // ---- O += V^T P; a masked block's infinite or undefined values may only reach the rows that see them: taken out here, added below ----
-      bool odd = false;
-      if constexpr (BF16) {
-        uint4 pf[2];
+    }
+    // ---- O += V^T P; a masked block's infinite or undefined values may only reach the rows that see them: taken out here, added below ----
+    bool odd = false;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-          pf[kk] = make_uint4(pack_bf16(s[8 * kk], s[8 * kk + 1]), pack_bf16(s[8 * kk + 2], s[8 * kk + 3]), pack_bf16(s[8 * kk + 4], s[8 * kk + 5]), pack_bf16(s[8 * kk + 6], s[8 * kk + 7]));
+    for (int u = 0; u < NB; ++u) {
+      if constexpr (BF16) {
         const int i16 = lane & 15, g16 = (lane >> 4) & 1;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+        for (int kk = 0; kk < 2; ++kk) {
+          const uint4 pf = make_uint4(pack_bf16(s[u][8 * kk], s[u][8 * kk + 1]), pack_bf16(s[u][8 * kk + 2], s[u][8 * kk + 3]), pack_bf16(s[u][8 * kk + 4], s[u][8 * kk + 5]),
+                                      pack_bf16(s[u][8 * kk + 6], s[u][8 * kk + 7]));
+          uint4 vf[CT];
 #pragma unroll
-          for (int c = 0; c < CT; ++c) {
-            uint4 vf;
+          for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
-              const int r = 32 * kb + 16 * kk + 8 * jj + 4 * half + (i16 >> 2);
+              const int r = 32 * (kb + u * KS) + 16 * kk + 8 * jj + 4 * half + (i16 >> 2);
               const char *from = reinterpret_cast<const char *>(values + VT::slot(r, 4 * c + 2 * g16 + ((i16 & 3) >> 1))) + 8 * (i16 & 1);
               const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
-              __builtin_memcpy(reinterpret_cast<char *>(&vf) + 8 * jj, &v, 8);
+              __builtin_memcpy(reinterpret_cast<char *>(&vf[c]) + 8 * jj, &v, 8);
             }
-            if (masked) {
-              unsigned *w = reinterpret_cast<unsigned *>(&vf);
+          if constexpr (MASKED) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+              unsigned *w = reinterpret_cast<unsigned *>(&vf[c]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const bool hi = (w[e] & 0x7f800000u) == 0x7f800000u, lo = (w[e] & 0x7f80u) == 0x7f80u;
@@ -220,23 +231,29 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
                 w[e] = (hi ? 0u : w[e] & 0xffff0000u) | (lo ? 0u : w[e] & 0xffffu);
               }
             }
-            mma_chunk<true>(o[c], vf, pf[kk]);
           }
+
+#pragma unroll
+          for (int c = 0; c < CT; ++c) mma_chunk<true>(o[c], vf[c], pf);
+
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
-            float v = reinterpret_cast<const float *>(values + VT::slot(32 * kb + acc_row(i, half), 8 * c + (n >> 2)))[n & 3];
-            if (masked) {
+            float v = reinterpret_cast<const float *>(values + VT::slot(32 * (kb + u * KS) + acc_row(i, half), 8 * c + (n >> 2)))[n & 3];
+            if constexpr (MASKED) {
               const bool bad = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
               odd |= bad;
               v = bad ? 0.f : v;
             }
-            o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], o[c], 0, 0, 0);
+            o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[u][i], o[c], 0, 0, 0);
           }
       }
-      if (masked && __any(odd)) {
+    }
+    if constexpr (MASKED) {
+      if (__any(odd)) {
 #pragma unroll 1
         for (int j = 0; j < 32; ++j) {
           if (key0 + j >= L) break;
@@ -253,6 +270,22 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
         }
       }
     }
+  };
+
+  request(0);
+  for (int t = 0; t < ntiles; ++t) {
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's part of tile t has landed
+    __syncthreads();                // ... and everybody else's; tile t-1 is no longer read
+    if (t + 1 < ntiles) request(t + 1);
+    // blocks of 32 keys: those that all of the wave's rows see whole, two at a time, then the others, one by one
+    const int full = min(max((w_first + 1 - t * KT) >> 5, 0), KT / 32);
+    int kb = ks;
+#pragma unroll 1
+    for (; kb + KS < full; kb += 2 * KS) blocks(std::integral_constant<int, 2>{}, std::false_type{}, t, kb);
+#pragma unroll 1
+    for (; kb < full; kb += KS) blocks(std::integral_constant<int, 1>{}, std::false_type{}, t, kb);
+#pragma unroll 1
+    for (; kb < KT / 32 && t * KT + 32 * kb <= w_last; kb += KS) blocks(std::integral_constant<int, 1>{}, std::true_type{}, t, kb);
   }
 
   // ---- fold the half-waves, then the waves with the same rows; out through LDS, whole rows ----
