@@ -307,10 +307,11 @@ __device__ __forceinline__ float group_sum(float v) {
 // warns about any such entry; the entry is still what orders its own M0 writes around this one).
 // The caller waits with s_waitcnt vmcnt(0) and a barrier before reading the data.
 typedef __attribute__((address_space(3))) void lds_void;
-template <int BYTES>
-__device__ __forceinline__ void load_to_lds(const void *base, unsigned byte_off, void *lds_base) {
+// .. to the LDS address itself
+template <int BYTES = 16>
+__device__ __forceinline__ void load_to_lds_at(const void *base, unsigned byte_off, unsigned lds_base) {
   static_assert(BYTES == 4 || BYTES == 16, "one dword or four per lane");
-  const unsigned lds_addr = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void *)lds_base);
+  const unsigned lds_addr = __builtin_amdgcn_readfirstlane(lds_base);
   // the base goes through the first lane's copy of it: free when it already sits in scalar registers,
   // and it keeps the operand a scalar pair when the compiler has lost track of its uniformity
   const unsigned long long bits = (unsigned long long)(uintptr_t)base;
@@ -323,6 +324,11 @@ __device__ __forceinline__ void load_to_lds(const void *base, unsigned byte_off,
   else
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(byte_off), "s"(base), "s"(lds_addr) : "memory", "m0");
 #pragma clang diagnostic pop
+}
+
+template <int BYTES>
+__device__ __forceinline__ void load_to_lds(const void *base, unsigned byte_off, void *lds_base) {
+  load_to_lds_at<BYTES>(base, byte_off, (unsigned)(uintptr_t)(lds_void *)lds_base);
 }
 
 // Rows of one (sequence, kv head, layer) by token, as 16-byte chunks; a row that is not wanted comes as zeros and costs no traffic.
@@ -425,13 +431,13 @@ __device__ __forceinline__ int lane_id_here() {
 // padding, so that one chunk column of 16 consecutive rows falls on 16 different 16-byte columns of the banks.
 // The permutation touches the two low bits of the chunk number only: a lane needs two base addresses, for
 // even and odd fragments, and everything else is an immediate offset.
-template <bool BF16, int D>
+template <bool BF16, int D, int ROWS = Cfg<BF16, D>::NCH == 32 ? 64 : 128>
 struct KeyTile {
   static constexpr int NCH = Cfg<BF16, D>::NCH;
   static_assert(NCH == 8 || NCH == 16 || NCH == 32, "rows of 128, 256 or 512 bytes");
   static constexpr int kGroup = 64 / NCH;
   static constexpr int kGroupChunks = 64 + (NCH == 32 ? 2 : 4);
-  static constexpr int kRows = NCH == 32 ? 64 : 128;
+  static constexpr int kRows = ROWS;
   static constexpr int kChunks = kRows / kGroup * kGroupChunks;
   __device__ static __forceinline__ int permute(int row_in_group) { return NCH == 8 ? row_in_group >> 1 : row_in_group; }
   // bytes from a tile's start to chunk 2 * odd + half of row n (n < 32); fragment f of block kb of 32 rows lies

@@ -65,6 +65,124 @@ __device__ __forceinline__ int reach_of(const PromptArgs &a, ScalarInts meta, co
   return min(r, L - 1);
 }
 
+// A wave's share of the call: the rows p0 .. p0 + 31 of query head h, and the keys that they see.
+struct PromptWave {
+  int l, gkv, h, tok, L, p0, ks;  // ks: of KS waves with the same rows, this one takes every KS-th block of 32 keys, from block ks on
+  int limit;                      // last key of this lane's row
+  int first, last, wg_last;       // last key of the first and of the last of the wave's rows (-1: no rows), and of the workgroup's last one
+};
+
+template <int KS>
+__device__ __forceinline__ PromptWave prompt_wave(const PromptArgs &a, ScalarInts meta) {
+  PromptWave w;
+  // groups of units, a group's units in turn, late positions (long key streams) first
+  const int units = a.n_layers * a.Hkv, u0 = blockIdx.x / (a.group * a.wgs_total) * a.group, n_group = min(a.group, units - u0);
+  const int rest = blockIdx.x - u0 * a.wgs_total, turn = rest / n_group, unit = u0 + rest - turn * n_group, x = a.wgs_total - 1 - turn;
+  w.l = unit / a.Hkv;
+  w.gkv = unit - w.l * a.Hkv;
+  int b = 0;
+  for (int lo = 0, hi = meta[PW_BATCH]; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (meta[PW_HEADER + mid * PS_WORDS + PS_WG] <= x) b = lo = mid; else hi = mid;
+  }
+  const ScalarInts rec = meta + PW_HEADER + b * PS_WORDS;
+  const int prefix = rec[PS_PREFIX], span0 = rec[PS_SPAN], n_spans = rec[PS_N_SPANS];
+  w.L = rec[PS_L];
+  w.tok = rec[PS_TOK];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = threadIdx.x & 31;
+  // item i of the sequence: head i % G of the kv group, query rows [32 * (i / G), + 32)
+  const int items = (w.L + kPromptRows - 1) / kPromptRows * a.G;
+  constexpr int kItems = kPromptWaves / KS;
+  w.ks = wave / kItems;
+  const int first = (x - rec[PS_WG]) * kItems, mine = first + wave - w.ks * kItems, item = min(mine, items - 1), pb = item / a.G;
+  w.h = w.gkv * a.G + (item - pb * a.G);
+  w.p0 = pb * kPromptRows;
+  const int wg_row = min((min(first + kItems, items) - 1) / a.G * kPromptRows + kPromptRows, w.L) - 1;
+  w.wg_last = __builtin_amdgcn_readfirstlane(reach_of(a, meta, w.L, prefix, span0, n_spans, wg_row));
+  w.limit = reach_of(a, meta, w.L, prefix, span0, n_spans, min(w.p0 + n, w.L - 1));
+  w.first = __builtin_amdgcn_readfirstlane(w.limit);
+  w.last = mine < items ? __builtin_amdgcn_readlane(w.limit, 31) : -1;
+  return w;
+}
+
+// The rows' outputs o [channel][row], maxima and sums (z: of either half-wave's keys) of the KS waves that share them, folded and stored by whole rows.
+// Every wave of the workgroup calls.
+template <bool BF16, int D, int KS>
+__device__ __forceinline__ void store_rows(const PromptArgs &a, const PromptWave &w, const f32x16_t (&o)[D / 32], float m, float z, float *lds) {
+  constexpr int NCH = Cfg<BF16, D>::NCH, EPC = Cfg<BF16, D>::kElemsPerChunk, kItems = kPromptWaves / KS;
+  constexpr int SS = D + 4;  // row of a wave's output in LDS: D channels, m, z
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+  z += __shfl_xor(z, 32, 64);
+  __syncthreads();  // nobody reads tiles any more
+  float *st = lds + wave * 32 * SS;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<float4 *>(st + n * SS + 32 * c + acc_row(i, half)) = make_float4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
+  if (half == 0) { st[n * SS + D] = m; st[n * SS + D + 1] = z; }
+  __syncthreads();
+  if (w.last < 0) return;
+  uint4 *out = reinterpret_cast<uint4 *>(a.out) + (long long)w.l * a.qs_layer + (long long)w.h * a.qs_head + (long long)(w.tok + w.p0) * a.qs_tok;
+  const float *st0 = lds + (wave - w.ks * kItems) * 32 * SS;
+  // the waves of the rows store a share of them each
+#pragma unroll 1
+  for (int r = w.ks * (32 / KS) + lane / NCH; r < (w.ks + 1) * (32 / KS); r += 64 / NCH) {
+    if (w.p0 + r >= w.L) break;
+    float M = -FLT_MAX, zz = 0.f, f[EPC];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) M = fmaxf(M, st0[(i * kItems * 32 + r) * SS + D]);
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) f[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const float *row = st0 + (i * kItems * 32 + r) * SS;
+      const float g = fast_exp2(row[D] - M);
+      zz = fmaf(row[D + 1], g, zz);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) f[e] = fmaf(row[lane % NCH * EPC + e], g, f[e]);
+    }
+    const float inv = 1.f / zz;
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) f[e] *= inv;
+    out[r * a.qs_tok + lane % NCH] = floats_to_chunk<BF16>(f);
+  }
+}
+
+// log2-domain scores of the products s[first .. first + N - 1] of row q with the keys key + acc_row(i, 0) (key: of this lane's half)
+template <bool SCORED, int N, bool FINE = false>
+__device__ __forceinline__ void score(const PromptArgs &a, f32x16_t &s, int first, float slope, int key, int q) {
+#pragma clang fp contract(off)
+  if (SCORED && a.score.cap > 0.f) {
+#pragma unroll
+    for (int i = first; i < first + N; ++i) s[i] = capped<FINE>(a.score, s[i]);
+  } else {
+#pragma unroll
+    for (int i = first; i < first + N; ++i) s[i] *= a.score.cl;
+  }
+  if (SCORED && a.score.slopes) {
+#pragma unroll
+    for (int i = first; i < first + N; ++i) s[i] = fmaf(-slope, fabsf((float)(key - q + acc_row(i, 0))), s[i]);
+  }
+}
+
+// exp2(s - m), s a rounded score.  (Not a fused multiply-add of the product: what that keeps of a product's rounding is 2^-24 of it, and logits may be 1e30.)
+__device__ __forceinline__ float weight(float s, float m) {
+#pragma clang fp contract(off)
+  return fast_exp2(s - m);
+}
+
+// (an LDS address is 32 bits wide; the cast goes through uintptr_t for the host's pass over this file)
+template <class T>
+__device__ __forceinline__ const __attribute__((address_space(3))) T *lds_at(unsigned at) {
+  return (const __attribute__((address_space(3))) T *)(uintptr_t)at;
+}
+__device__ __forceinline__ uint4 lds_chunk(unsigned at) {
+  typedef __attribute__((ext_vector_type(4))) unsigned u32x4_t;
+  const u32x4_t v = *lds_at<u32x4_t>(at);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 template <bool BF16, int D, int KS, bool SCORED>
 __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelArgs<PromptArgs> k) {
   const PromptArgs &a = k.a;
@@ -77,41 +195,20 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
   extern __shared__ __align__(16) uint4 lds_kv[];  // [2] K tile, V tile; at the end the waves' outputs
 
   const ScalarInts meta = first_meta(k, a.meta);
-  // groups of units, a group's units in turn, late positions (long key streams) first
-  const int units = a.n_layers * a.Hkv, u0 = blockIdx.x / (a.group * a.wgs_total) * a.group, n_group = min(a.group, units - u0);
-  const int rest = blockIdx.x - u0 * a.wgs_total, turn = rest / n_group, unit = u0 + rest - turn * n_group, x = a.wgs_total - 1 - turn;
-  const int l = unit / a.Hkv, gkv = unit - l * a.Hkv;
-  int b = 0;
-  for (int lo = 0, hi = meta[PW_BATCH]; hi - lo > 1;) {
-    const int mid = (lo + hi) >> 1;
-    if (meta[PW_HEADER + mid * PS_WORDS + PS_WG] <= x) b = lo = mid; else hi = mid;
-  }
-  const ScalarInts rec = meta + PW_HEADER + b * PS_WORDS;
-  const int L = rec[PS_L], tok = rec[PS_TOK], prefix = rec[PS_PREFIX], span0 = rec[PS_SPAN], n_spans = rec[PS_N_SPANS];
+  const PromptWave w = prompt_wave<KS>(a, meta);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
-  // item i of the sequence: head i % G of the kv group, query rows [32 * (i / G), + 32)
-  const int items = (L + kPromptRows - 1) / kPromptRows * a.G;
-  constexpr int kItems = kPromptWaves / KS;
-  const int ks = wave / kItems;  // this wave takes every KS-th block of 32 keys, from block ks on
-  const int first = (x - rec[PS_WG]) * kItems, mine = first + wave - ks * kItems, item = min(mine, items - 1);
-  const bool active = mine < items;
-  const int pb = item / a.G, h = gkv * a.G + (item - pb * a.G), p0 = pb * kPromptRows;
-  const int wg_row = min((min(first + kItems, items) - 1) / a.G * kPromptRows + kPromptRows, L) - 1;  // last row of the workgroup
-  const int wg_last = __builtin_amdgcn_readfirstlane(reach_of(a, meta, L, prefix, span0, n_spans, wg_row));
-  const int limit = reach_of(a, meta, L, prefix, span0, n_spans, min(p0 + n, L - 1));  // of this lane's row
-  const int w_first = __builtin_amdgcn_readfirstlane(limit), w_last = active ? __builtin_amdgcn_readlane(limit, 31) : -1;
+  const int L = w.L, p0 = w.p0, ks = w.ks, limit = w.limit, w_first = w.first, w_last = w.last;
 
   // ---- this wave's query rows (clamped past the end of the sequence), through its share of the LDS ----
   uint4 qf[NF];
-  const uint4 *Q = reinterpret_cast<const uint4 *>(a.Q) + (long long)l * a.qs_layer + (long long)h * a.qs_head + (long long)(tok + p0) * a.qs_tok;
+  const uint4 *Q = reinterpret_cast<const uint4 *>(a.Q) + (long long)w.l * a.qs_layer + (long long)w.h * a.qs_head + (long long)(w.tok + p0) * a.qs_tok;
   static_assert(kPromptWaves * 32 * NCH <= 2 * kBuffer, "the waves' query rows");
   fetch_rows_staged<BF16, D>(Q, (unsigned)a.qs_tok, min(p0 + n, L - 1) - p0, lds_kv + wave * 32 * NCH, qf);
   __syncthreads();  // the tiles may overwrite the other waves' shares now
 
-  const long long kv_at = (long long)l * a.ks_layer + (long long)gkv * a.ks_head + (long long)tok * a.ks_tok;
+  const long long kv_at = (long long)w.l * a.ks_layer + (long long)w.gkv * a.ks_head + (long long)w.tok * a.ks_tok;
   const uint4 *K = reinterpret_cast<const uint4 *>(a.K) + kv_at, *V = reinterpret_cast<const uint4 *>(a.V) + kv_at;
-  const float cl = a.score.cl;
-  const float slope = SCORED && a.score.slopes ? a.score.slopes[h] * 1.4426950408889634f : 0.f;
+  const float slope = SCORED && a.score.slopes ? a.score.slopes[w.h] * 1.4426950408889634f : 0.f;
   float m = -FLT_MAX, z = 0.f;  // of row n; z over the keys of this half-wave
   f32x16_t o[CT];               // [channel 32 c + ..][row n]
 #pragma unroll
@@ -119,66 +216,114 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
 
-  const int ntiles = wg_last / KT + 1;
+  const int ntiles = w.wg_last / KT + 1;
+  // Requests of a tile: this wave's share of its rows.  Whole tiles whose rows lie within 4 GiB (nearly all) by offsets from the tile's first row that stay the same.
+  constexpr int kKLoads = KT / TL::kGroup / kPromptWaves, kVLoads = KT / VT::RPI / kPromptWaves;
+  const bool near = a.ks_tok < (1ll << 32) / (16 * KT);
+  unsigned k_off[kKLoads], v_off[kVLoads];
+#pragma unroll
+  for (int i = 0; i < kKLoads; ++i) {
+    const int j = lane / NCH, r = (i * kPromptWaves + wave) * TL::kGroup + j;
+    k_off[i] = ((unsigned)r * (unsigned)a.ks_tok + (unsigned)((lane % NCH) ^ TL::permute(j))) * 16u;
+  }
+#pragma unroll
+  for (int i = 0; i < kVLoads; ++i) {
+    const int r = (i * kPromptWaves + wave) * VT::RPI + lane / NCH;
+    v_off[i] = ((unsigned)r * (unsigned)a.ks_tok + (unsigned)((lane % NCH) ^ VT::permute(r))) * 16u;
+  }
+  const unsigned lds0 = (unsigned)(uintptr_t)(lds_void *)lds_kv;
   auto request = [&](int t) {
-    uint4 *to = lds_kv + (t & 1) * kBuffer;
-    TL::template request<kPromptWaves>(K, a.ks_tok, t * KT, L - 1, to, wave);
-    VT::template request<kPromptWaves>(V, a.ks_tok, t * KT, L - 1, to + TL::kChunks, wave);
+    if (near && (t + 1) * KT <= L) {
+      const long long skip = (long long)(t * KT) * a.ks_tok;
+      const uint4 *kt = K + skip, *vt = V + skip;
+      const unsigned to = lds0 + (t & 1) * kBuffer * 16;
+#pragma unroll
+      for (int i = 0; i < kKLoads; ++i) load_to_lds_at(kt, k_off[i], to + (i * kPromptWaves + wave) * TL::kGroupChunks * 16);
+#pragma unroll
+      for (int i = 0; i < kVLoads; ++i) load_to_lds_at(vt, v_off[i], to + (TL::kChunks + (i * kPromptWaves + wave) * 64) * 16);
+    } else {
+      uint4 *to = lds_kv + (t & 1) * kBuffer;
+      TL::template request<kPromptWaves>(K, a.ks_tok, t * KT, L - 1, to, wave);
+      VT::template request<kPromptWaves>(V, a.ks_tok, t * KT, L - 1, to + TL::kChunks, wave);
+    }
   };
+  const unsigned k_frag[2] = {(unsigned)TL::frag_offset(n, half, 0), (unsigned)TL::frag_offset(n, half, 1)};  // bytes from the start of a K tile
+  unsigned v_frag[CT];  // .. of a V tile, to this lane's share of the four rows that 16 lanes transpose
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int i16 = lane & 15, g16 = (lane >> 4) & 1;
+    v_frag[c] = BF16 ? (unsigned)(VT::slot(4 * half + (i16 >> 2), 4 * c + 2 * g16 + ((i16 & 3) >> 1)) * 16 + 8 * (i16 & 1)) : 0u;
+  }
   // blocks kb, kb + KS, .. (NB of them) of tile t; MASKED: some row of the wave does not see all of their keys
   auto blocks = [&](auto nb, auto masked_t, int t, int kb) __attribute__((always_inline)) {
     constexpr int NB = decltype(nb)::value;
     constexpr bool MASKED = decltype(masked_t)::value;
-    const char *tile = reinterpret_cast<const char *>(lds_kv + (t & 1) * kBuffer);
-    const char *rows0 = tile + TL::frag_offset(n, half, 0), *rows1 = tile + TL::frag_offset(n, half, 1);
-    const uint4 *values = lds_kv + (t & 1) * kBuffer + TL::kChunks;
+    // LDS addresses of this lane's shares, one a register (opaque: the compiler would keep and advance one for every read)
+    const unsigned tile = lds0 + (t & 1) * kBuffer * 16, values = tile + TL::kChunks * 16;
+    unsigned k_at[2], v_at[BF16 ? CT : 1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      k_at[i] = tile + k_frag[i] + kb * TL::block_bytes(1);
+      asm volatile("" : "+v"(k_at[i]));
+    }
+#pragma unroll
+    for (int c = 0; c < (BF16 ? CT : 1); ++c) {
+      v_at[c] = values + v_frag[c] + kb * 32 * NCH * 16;
+      asm volatile("" : "+v"(v_at[c]));
+    }
     const int key0 = t * KT + 32 * kb;
     f32x16_t s[NB];  // [key][row]
-#pragma unroll
-    for (int u = 0; u < NB; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
 
+    // K fragments asked for 3 steps ahead (pinned: left to itself the compiler reads each one right before its use)
+    constexpr int kAhead = NF < 3 ? NF : 3;
+    uint4 kf[NF][NB];
+    auto read_k = [&](int f) {
 #pragma unroll
-    for (int f = 0; f < NF; ++f)
+      for (int u = 0; u < NB; ++u) kf[f][u] = lds_chunk(k_at[f & 1] + u * KS * TL::block_bytes(1) + 64 * (f >> 1));
+    };
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) read_k(f);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
 #pragma unroll
       for (int u = 0; u < NB; ++u) {
-        const uint4 kf = *reinterpret_cast<const uint4 *>((f & 1 ? rows1 : rows0) + (kb + u * KS) * TL::block_bytes(1) + 64 * (f >> 1));
-        mma_chunk<BF16>(s[u], kf, qf[f]);
+        if (f == 0) s[u] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        mma_chunk<BF16>(s[u], kf[f][u], qf[f]);
       }
-
+      if (f + kAhead < NF) read_k(f + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     // ---- scores ----
+    auto most = [&]() {
+      float x = fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+      for (int u = 0; u < NB; ++u)
+#pragma unroll
+        for (int i = u ? 0 : 2; i < 16; i += 2) x = fmaxf(fmaxf(x, s[u][i]), s[u][i + 1]);
+      return x;
+    };
+    // Whole blocks: weights exp2(fma(product, scale, -maximum)), which keeps what the maximum's own rounding lost, 2^-24 of it: nothing where scores are
+    // within 2^24, an overflow at 1e30.  Larger ones (or NaN) are rounded first, as everywhere else.
+    float mul = 1.f, tm = 0.f;
+    bool fused = !MASKED && !SCORED;
+    if constexpr (!MASKED && !SCORED) {
+      tm = most();
+      fused = !__any(!(fabsf(tm) * a.score.cl < 0x1p24f));
+      if (fused) { mul = a.score.cl; tm *= mul; }
+    }
+    if (!fused) {
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
-      if constexpr (SCORED) {
-        if (a.score.cap > 0.f) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] = capped<!BF16>(a.score, s[u][i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] *= cl;
-        }
-        if (a.score.slopes) {
-          const int ahead = key0 + 32 * u * KS + 4 * half - (p0 + n);  // of key 0 of this lane
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] = fmaf(-slope, fabsf((float)(ahead + acc_row(i, 0))), s[u][i]);
-        }
-      } else {
-        // (rounded here, not by a fused multiply-add with the maximum below: what that leaves of a product's rounding is 2^-24 of it, and logits may be 1e30)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][i] *= cl;
-      }
+      score<SCORED, 16, !BF16>(a, s[u], 0, slope, key0 + 32 * u * KS + 4 * half, p0 + n);
       if constexpr (MASKED) {
         const int last = limit - key0 - 32 * u * KS - 4 * half;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[u][i] = acc_row(i, 0) <= last ? s[u][i] : -INFINITY;
       }
     }
-    float tm = fmaxf(s[0][0], s[0][1]);
-#pragma unroll
-    for (int u = 0; u < NB; ++u)
-#pragma unroll
-      for (int i = u ? 0 : 2; i < 16; i += 2) tm = fmaxf(fmaxf(tm, s[u][i]), s[u][i + 1]);
+    tm = most();
+    }
     if (__any(tm > m + kLazy)) {
       const float M = fmaxf(m, fmaxf(tm, __shfl_xor(tm, 32, 64))), f = fast_exp2(m - M);
       z *= f;
@@ -193,8 +338,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
       float za = 0.f, zb = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        s[u][i] = fast_exp2(s[u][i] - m);
-        s[u][i + 1] = fast_exp2(s[u][i + 1] - m);
+        s[u][i] = !MASKED && !SCORED ? fast_exp2(fmaf(s[u][i], mul, -m)) : weight(s[u][i], m);
+        s[u][i + 1] = !MASKED && !SCORED ? fast_exp2(fmaf(s[u][i + 1], mul, -m)) : weight(s[u][i + 1], m);
         za += s[u][i];
         zb += s[u][i + 1];
       }
@@ -205,7 +350,6 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
       if constexpr (BF16) {
-        const int i16 = lane & 15, g16 = (lane >> 4) & 1;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           const uint4 pf = make_uint4(pack_bf16(s[u][8 * kk], s[u][8 * kk + 1]), pack_bf16(s[u][8 * kk + 2], s[u][8 * kk + 3]), pack_bf16(s[u][8 * kk + 4], s[u][8 * kk + 5]),
@@ -215,9 +359,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
           for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
-              const int r = 32 * (kb + u * KS) + 16 * kk + 8 * jj + 4 * half + (i16 >> 2);
-              const char *from = reinterpret_cast<const char *>(values + VT::slot(r, 4 * c + 2 * g16 + ((i16 & 3) >> 1))) + 8 * (i16 & 1);
-              const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)from);
+              const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)lds_at<s16x4_t>(v_at[c] + (32 * u * KS + 16 * kk + 8 * jj) * NCH * 16));
               __builtin_memcpy(reinterpret_cast<char *>(&vf[c]) + 8 * jj, &v, 8);
             }
           if constexpr (MASKED) {
@@ -242,7 +384,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
         for (int i = 0; i < 16; ++i)
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
-            float v = reinterpret_cast<const float *>(values + VT::slot(32 * (kb + u * KS) + acc_row(i, half), 8 * c + (n >> 2)))[n & 3];
+            float v = *lds_at<float>(values + VT::slot(32 * (kb + u * KS) + acc_row(i, half), 8 * c + (n >> 2)) * 16 + 4 * (n & 3));
             if constexpr (MASKED) {
               const bool bad = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
               odd |= bad;
@@ -263,8 +405,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
             for (int i = 0; i < 16; ++i) {
               const int ch = 32 * c + acc_row(i, half);
               float v;
-              if constexpr (BF16) v = bf16_bits_to_float(reinterpret_cast<const uint16_t *>(values + VT::slot(32 * kb + j, ch >> 3))[ch & 7]);
-              else v = reinterpret_cast<const float *>(values + VT::slot(32 * kb + j, ch >> 2))[ch & 3];
+              if constexpr (BF16) v = bf16_bits_to_float(*lds_at<uint16_t>(values + VT::slot(32 * kb + j, ch >> 3) * 16 + 2 * (ch & 7)));
+              else v = *lds_at<float>(values + VT::slot(32 * kb + j, ch >> 2) * 16 + 4 * (ch & 3));
               if (!(fabsf(v) < INFINITY) && key0 + j <= limit) o[c][i] += v;
             }
         }
@@ -281,51 +423,14 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
     const int full = min(max((w_first + 1 - t * KT) >> 5, 0), KT / 32);
     int kb = ks;
 #pragma unroll 1
-    for (; kb + KS < full; kb += 2 * KS) blocks(std::integral_constant<int, 2>{}, std::false_type{}, t, kb);
+    for (; BF16 && kb + KS < full; kb += 2 * KS) blocks(std::integral_constant<int, 2>{}, std::false_type{}, t, kb);
 #pragma unroll 1
     for (; kb < full; kb += KS) blocks(std::integral_constant<int, 1>{}, std::false_type{}, t, kb);
 #pragma unroll 1
     for (; kb < KT / 32 && t * KT + 32 * kb <= w_last; kb += KS) blocks(std::integral_constant<int, 1>{}, std::true_type{}, t, kb);
   }
 
-  // ---- fold the half-waves, then the waves with the same rows; out through LDS, whole rows ----
-  z += __shfl_xor(z, 32, 64);
-  __syncthreads();  // nobody reads tiles any more
-  constexpr int SS = D + 4;  // row of a wave's output in LDS: D channels, m, z
-  float *st = reinterpret_cast<float *>(lds_kv) + wave * 32 * SS;
-#pragma unroll
-  for (int c = 0; c < CT; ++c)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      *reinterpret_cast<float4 *>(st + n * SS + 32 * c + acc_row(i, half)) = make_float4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
-  if (half == 0) { st[n * SS + D] = m; st[n * SS + D + 1] = z; }
-  __syncthreads();
-  if (!active) return;
-  // the KS waves of the rows store a share of them each
-  constexpr int EPC = CF::kElemsPerChunk, RPT = 64 / NCH;
-  uint4 *out = reinterpret_cast<uint4 *>(a.out) + (long long)l * a.qs_layer + (long long)h * a.qs_head + (long long)(tok + p0) * a.qs_tok;
-  const float *st0 = reinterpret_cast<const float *>(lds_kv) + (wave - ks * kItems) * 32 * SS;
-#pragma unroll 1
-  for (int r = ks * (32 / KS) + lane / NCH; r < (ks + 1) * (32 / KS); r += RPT) {
-    if (p0 + r >= L) break;
-    float M = -FLT_MAX, zz = 0.f, f[EPC];
-#pragma unroll
-    for (int w = 0; w < KS; ++w) M = fmaxf(M, st0[(w * kItems * 32 + r) * SS + D]);
-#pragma unroll
-    for (int e = 0; e < EPC; ++e) f[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < KS; ++w) {
-      const float *row = st0 + (w * kItems * 32 + r) * SS;
-      const float g = fast_exp2(row[D] - M);
-      zz = fmaf(row[D + 1], g, zz);
-#pragma unroll
-      for (int e = 0; e < EPC; ++e) f[e] = fmaf(row[lane % NCH * EPC + e], g, f[e]);
-    }
-    const float inv = 1.f / zz;
-#pragma unroll
-    for (int e = 0; e < EPC; ++e) f[e] *= inv;
-    out[r * a.qs_tok + lane % NCH] = floats_to_chunk<BF16>(f);
-  }
+  store_rows<BF16, D, KS>(a, w, o, m, z, reinterpret_cast<float *>(lds_kv));
 }
 
 template <bool BF16, int D, int KS, bool SCORED>
