@@ -15,6 +15,7 @@
 //             (ds_read_b64_tr_b8, _tr_b16), in the order of keys in which the accumulators of S hold p.
 // Rows past a sequence's end are read as its last one; their p is 0 and so are their V, whatever that row holds.
 #include <cfloat>
+#include <cmath>
 
 #include "attention_core.h"
 #include "decode_core.h"
@@ -71,8 +72,8 @@ __device__ __forceinline__ s16x4_t pack_upper(const unsigned (&v)[4]) {
   return r;
 }
 
-// grid (tasks, kv heads, layers)
-template <int R, bool QBF16, int D, int WAVES, bool POS>
+// a task per workgroup (decode_task)
+template <int R, bool QBF16, int D, int WAVES, bool POS, bool ORDERED>
 __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attention_kernel(CacheAttnArgs a) {
   using RC = RowCfg<R, D>;
   constexpr int NCH = RC::NCH, TR = RC::kRows, SUBS = RC::kSubs, DT = D / 16;
@@ -80,14 +81,9 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
   constexpr int kTerms = QBF16 ? 2 : 3;  // of p
   constexpr int KJ = R == kRowF32 ? NCH / 4 : R == kRowBF16 ? NCH / 4 : NCH / 4;  // chunks of a row in a lane
   extern __shared__ __align__(16) uint4 lds_rows[];  // [waves] K tile, V tile, positions; at the end the waves' states
-  const int x = blockIdx.x, gkv = blockIdx.y, l = blockIdx.z;
-  int b = 0;
-  for (int lo = 0, hi = a.n_seqs; hi - lo > 1;) {
-    const int mid = (lo + hi) >> 1;
-    if (a.seq[mid].task <= x) b = lo = mid; else hi = mid;
-  }
-  const auto &s = a.seq[b];
-  const int len = s.len, s0 = (x - s.task) * a.chunk, s1 = min(len, s0 + a.chunk);
+  const DecodeTask task = decode_task<ORDERED>(a);
+  const int b = task.b, x = task.x, gkv = task.gkv, l = task.l, len = task.B, s0 = task.s0, s1 = task.s1;
+  const auto &s = a.cu[b];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q4 = lane >> 4;
   const long long unit = (long long)l * a.Hkv + gkv;
   const long long seq_at = l * a.ks_layer + gkv * a.ks_head + (long long)s.row * a.ks_tok;
@@ -367,7 +363,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
 template <bool QBF16, int D>
 __global__ __launch_bounds__(D) void cache_attention_combine_kernel(CacheAttnArgs a) {
   const int b = blockIdx.x;
-  const int x0 = a.seq[b].task, x1 = a.seq[b + 1].task;
+  const int x0 = a.cu[b].task & 0xffff, x1 = a.cu[b + 1].task & 0xffff;
   if (x1 - x0 < 2) return;
   const long long head = (long long)blockIdx.z * a.Hq + blockIdx.y;
   const int ci = threadIdx.x;
@@ -390,19 +386,28 @@ hipError_t launch_waves(const CacheAttnArgs &a, int n_layers, hipStream_t stream
   size_t lds = (size_t)WAVES * (2 * RC::kChunks + (a.row_pos ? 16 : 0)) * 16;
   const size_t states = (size_t)WAVES * nh * (D + 4) * sizeof(float);
   if (states > lds) lds = states;
-  const hipError_t e = allow_full_lds<cache_attention_kernel<R, QBF16, D, WAVES, false>, cache_attention_kernel<R, QBF16, D, WAVES, true>>();
+  const hipError_t e = allow_full_lds<cache_attention_kernel<R, QBF16, D, WAVES, false, false>, cache_attention_kernel<R, QBF16, D, WAVES, true, false>,
+                                      cache_attention_kernel<R, QBF16, D, WAVES, false, true>, cache_attention_kernel<R, QBF16, D, WAVES, true, true>>();
   if (e != hipSuccess) return e;
   ProfScope ps(stream, KID_CACHE_ATTENTION);
-  const dim3 grid(a.tasks, a.Hkv, n_layers);
-  if (a.row_pos) cache_attention_kernel<R, QBF16, D, WAVES, true><<<grid, WAVES * 64, lds, stream>>>(a);
-  else cache_attention_kernel<R, QBF16, D, WAVES, false><<<grid, WAVES * 64, lds, stream>>>(a);
+  if (a.mixed < 0) {
+    const dim3 grid(a.tasks, a.Hkv, n_layers);
+    if (a.row_pos) cache_attention_kernel<R, QBF16, D, WAVES, true, false><<<grid, WAVES * 64, lds, stream>>>(a);
+    else cache_attention_kernel<R, QBF16, D, WAVES, false, false><<<grid, WAVES * 64, lds, stream>>>(a);
+  } else {
+    const dim3 grid(a.Hkv, n_layers, a.tasks);
+    if (a.row_pos) cache_attention_kernel<R, QBF16, D, WAVES, true, true><<<grid, WAVES * 64, lds, stream>>>(a);
+    else cache_attention_kernel<R, QBF16, D, WAVES, false, true><<<grid, WAVES * 64, lds, stream>>>(a);
+  }
   return hipGetLastError();
 }
+
+constexpr int kMostWaves = 8;
 
 template <int R, bool QBF16, int D>
 hipError_t launch_rows(CacheAttnArgs a, int n_layers, hipStream_t stream) {
   for (a.g0 = 0; a.g0 < a.G; a.g0 += kAHeads) {
-    const hipError_t e = launch_waves<R, QBF16, D, R == kRowF32 ? 4 : 8>(a, n_layers, stream);
+    const hipError_t e = a.waves == 2 ? launch_waves<R, QBF16, D, 2>(a, n_layers, stream) : a.waves == 4 ? launch_waves<R, QBF16, D, 4>(a, n_layers, stream) : launch_waves<R, QBF16, D, kMostWaves>(a, n_layers, stream);
     if (e != hipSuccess) return e;
   }
   if (a.tasks > a.n_seqs) {
@@ -419,39 +424,77 @@ hipError_t launch_dim(const CacheAttnArgs &a, const CacheAttnCall &c, hipStream_
   return c.bf16 ? launch_rows<kRowFp8, true, D>(a, c.n_layers, stream) : launch_rows<kRowFp8, false, D>(a, c.n_layers, stream);
 }
 
-// Rows of a task.
-int rows_of_task(const CacheAttnCall &c, int Hkv, int b0, int n_seqs) {
-  long long rows = 0;
+// Rows of a task and waves of a workgroup for the sequences of a launch.
+//
+// A workgroup alone on its compute unit takes a trip of its eight waves over its rows in `trip` us (measured at 128 channels; 0.8 of it at 64); 224 of them (fp32 256)
+// reach the memory's rate.  Fewer (counted as sequences of the longest one's length) are cut into about as many parts, if the trips saved are worth the second
+// launch, 2.4 us and 0.25 a part, and into no more than the square root that balances the two.  Over 324 shapes of 1 to 512 units x 64 to 16000 equal rows this is
+// 1 % from the best of all cuts on average, over 75 unequal batches 2 %.  us, whole / cut: codes 112 units x 16000 rows 97 / 85 in two, x 1800 16.4 / 17.2; 64 x 8000
+// 46 / 30 in three; 16 x 3600 21.6 / 11.3 in six; 1 x 16000 80 / 16 in sixteen, x 450 6.5 / 7.7 in two; bf16 112 x 3600 47 / 42, 32 x 8000 77 / 31 in six, 256 x 900
+// 25.1 / 30.1; fp32 112 x 450 18.9 / 16.7, 32 x 900 30 / 14 in six.
+// Short sequences: where there are enough workgroups, fewer waves leave room for more of them (8 / 4 / 2 waves, codes 256 units x 64 rows 5.2 / - / 4.6, x 256 9.2 / 6.5 / -,
+// 512 x 450 16.9 / 15.6 / -; bf16 512 x 256 17.5 / - / 16.1; fp32 512 x 256 30.4 / 27.5 / 31.3, 16 x 900 uncut 25.8 / 30.4 / 53.5).
+void choose_tasks(CacheAttnArgs &a, const CacheAttnCall &c, const int *len) {
+  long long sum = 0;
   int longest = 0;
-  for (int i = 0; i < n_seqs; ++i) {
-    rows += c.lengths[b0 + i];
-    if (c.lengths[b0 + i] > longest) longest = c.lengths[b0 + i];
+  for (int i = 0; i < a.n_seqs; ++i) {
+    sum += len[i];
+    if (len[i] > longest) longest = len[i];
   }
-  long long chunk = (rows * c.n_layers * Hkv + kCacheAttnTasks - 1) / kCacheAttnTasks;
-  const int least = longest / kCacheAttnMostParts + 1 > kCacheAttnLeastPart ? longest / kCacheAttnMostParts + 1 : kCacheAttnLeastPart;
-  if (chunk < least) chunk = least;
-  if (chunk > longest) chunk = longest;
-  return (int)((chunk + kQuantRows - 1) / kQuantRows * kQuantRows);
+  const long long units = (long long)c.n_layers * a.Hkv, wgs = units * a.n_seqs;
+  const int tile = c.rows == kRowFp8 ? 32 : 16, rows = kMostWaves * tile;
+  const float trip = (c.rows == kRowFp8 ? 1.25f : c.rows == kRowBF16 ? 0.7f : 1.8f) * (c.d == 64 ? 0.8f : 1.f);
+  if (c.rows == kRowF32) a.waves = wgs >= 256 || longest <= 16 * tile ? 4 : kMostWaves;
+  else a.waves = (wgs >= 64 && longest <= 2 * tile) || (wgs >= 256 && longest <= 4 * tile) ? 2 : wgs >= 256 && longest <= 28 * tile ? 4 : kMostWaves;
+  long long chunk = longest;
+  if (longest > kCacheAttnLeastPart) {
+    const float room = c.rows == kRowF32 ? 256.f : 224.f;
+    int parts = (int)(room * longest / ((float)units * sum) + 0.45f), balance = (int)std::sqrt((float)longest / rows * trip * 4.f);
+    if (parts > balance) parts = balance;
+    if (parts > kCacheAttnMostParts) parts = kCacheAttnMostParts;
+    if (parts > 1) {
+      const long long part = (longest + parts - 1) / parts;
+      const int passes = (a.G + kAHeads - 1) / kAHeads;
+      const long long saved = (longest + rows - 1) / rows - (part + rows - 1) / rows;
+      if ((float)(saved * passes) * trip > 2.4f + 0.25f * parts) chunk = part;
+    }
+    // what the workspace has room for
+    long long least = (sum * units + kCacheAttnTasks - 1) / kCacheAttnTasks;
+    if (least < longest / kCacheAttnMostParts + 1) least = longest / kCacheAttnMostParts + 1;
+    if (least < kCacheAttnLeastPart) least = kCacheAttnLeastPart;
+    if (chunk < least) chunk = least;
+  }
+  if (chunk < kQuantRows) chunk = kQuantRows;
+  a.chunk = (int)((chunk + kQuantRows - 1) / kQuantRows * kQuantRows);
 }
 
 }  // namespace
 
 hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnCall &c, hipStream_t stream) {
   int block = 0, slot = 0;
-  for (a.b0 = 0; a.b0 < a.batch; a.b0 += kCacheAttnSeqs) {
-    a.n_seqs = a.batch - a.b0 < kCacheAttnSeqs ? a.batch - a.b0 : kCacheAttnSeqs;
-    a.chunk = rows_of_task(c, a.Hkv, a.b0, a.n_seqs);
-    if (a.chunk < kQuantRows) a.chunk = kQuantRows;
+  for (a.b0 = 0; a.b0 < a.batch; a.b0 += kDecodeSeqs) {
+    a.n_seqs = a.batch - a.b0 < kDecodeSeqs ? a.batch - a.b0 : kDecodeSeqs;
+    const int *len = c.lengths + a.b0;
+    choose_tasks(a, c, len);
     a.tasks = 0;
+    long long sum = 0;
+    int longest = 0;
     for (int i = 0; i < a.n_seqs; ++i) {
-      const int b = a.b0 + i, len = c.lengths[b];
+      const int b = a.b0 + i;
       const int merged = a.row_pos ? c.budgets[b] : 0;
-      a.seq[i] = CacheAttnArgs::Seq{a.tasks, len, c.cu_capacity[b], block, merged, slot, a.row_pos ? c.q_pos[b] : 0, 0};
-      a.tasks += len <= a.chunk ? 1 : (len + a.chunk - 1) / a.chunk;
+      a.cu[i] = CacheAttnArgs::Seq{a.tasks, len[i], c.cu_capacity[b], block, merged, slot, a.row_pos ? c.q_pos[b] : 0, 0};
+      a.tasks += len[i] <= a.chunk ? 1 : (len[i] + a.chunk - 1) / a.chunk;
       block += (c.cu_capacity[b + 1] - c.cu_capacity[b] + kQuantRows - 1) / kQuantRows;
       slot += merged;
+      sum += len[i];
+      if (len[i] > longest) longest = len[i];
     }
-    a.seq[a.n_seqs].task = a.tasks;
+    a.cu[a.n_seqs] = CacheAttnArgs::Seq{a.tasks, 0, 0, 0, 0, 0, 0, 0};
+    // An order of their own for unequal sequences' tasks, where that can matter (as decode attention, in tiles of the most waves)
+    const int units = a.Hkv * c.n_layers, tile = c.rows == kRowFp8 ? 32 : 16;
+    const long long wgs = (long long)units * a.tasks, above = wgs <= 1024 ? kMostWaves * tile : tile;
+    if (wgs > 256 && longest * (long long)a.n_seqs - sum >= above * a.n_seqs) order_tasks(a, len, units);
+    else a.mixed = -1;
     const hipError_t e = c.d == 128 ? launch_dim<128>(a, c, stream) : launch_dim<64>(a, c, stream);
     if (e != hipSuccess) return e;
   }

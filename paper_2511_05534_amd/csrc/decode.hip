@@ -25,73 +25,8 @@ namespace flowmm {
 
 namespace {
 
-constexpr int kDecodeTail = 1024;  // four per compute unit (512: 0 to 3 us slower, 2048 to all: 0 to 9)
 constexpr int kDThreads = 256;
 constexpr int kDWaves = kDThreads / 64;
-
-// The last sequence of the launch, lo .. hi - 1, whose task number from bit SHIFT on is not behind i.
-template <int SHIFT>
-__device__ __forceinline__ int seq_of(const DecodeArgs &a, int i, int lo, int hi) {
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.cu[mid].task >> SHIFT <= i) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
-struct DecodeTask {
-  int b, x, s0, s1, B;  // sequence of the launch, its task's number among all, the task's slots, the sequence's slots
-  int gkv, l;
-};
-
-// Workgroups are handed out in the order of the linear index, to the eight XCDs in turn.  The last units' tasks (kDecodeTail of them) go
-// from the longest to the shortest over all of these units: compute units that are done early take short ones, and what
-// starts last is shortest.  Before, units go one after the other, so that long streams cover the starts of short ones (all tasks from the
-// longest to the shortest: 1024 units x {72 .. 487} slots 184 us, 176 so), each one task further on: with eight tasks to a unit one
-// sequence would stay on one XCD.
-// Tasks of a unit in a row throughout -> this, us: 112 units x {160 .. 982} 57 -> 50 (58 with the fold that parts of 512 need), 224 x {529 ..
-// 2856} 332 -> 274, 1024 x 8 x {103 .. 291} 155 -> 119, x {99 .. 506} 276 -> 232, 896 x 5 x {127 .. 551} 146 -> 144.
-// ORDERED: all this.  It costs a workgroup two more dependent scalar loads than the plain grid (0.3 us), which calls keep that gain
-// nothing from it.
-template <bool ORDERED>
-__device__ __forceinline__ DecodeTask decode_task(const DecodeArgs &a) {
-  DecodeTask t;
-  int part;
-  if constexpr (!ORDERED) {  // grid (tasks, kv heads, layers)
-    t.x = blockIdx.x; t.gkv = blockIdx.y; t.l = blockIdx.z;
-    t.b = seq_of<0>(a, t.x, max(0, t.x - (a.tasks - a.n_seqs)), min(a.n_seqs, t.x + 1));  // (every sequence has a task: whole ones need no search)
-    part = t.x - a.cu[t.b].task;
-  } else {  // grid (kv heads, layers, tasks), read by its linear index
-    const unsigned lin = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x, units = gridDim.x * gridDim.y;
-    const unsigned tasks = (unsigned)a.tasks, first = (unsigned)a.mixed * tasks;
-    unsigned unit, i;
-    if (lin < first) {
-      unsigned turn;
-      unit = quotient(lin, tasks, a.inv_tasks, i);
-      quotient(unit, tasks, a.inv_tasks, turn);
-      i = i + turn < tasks ? i + turn : i + turn - tasks;
-    } else {
-      i = quotient(lin - first, units - (unsigned)a.mixed, a.inv_last, unit);
-      unit += (unsigned)a.mixed;
-    }
-    unsigned gkv;
-    t.l = (int)quotient(unit, gridDim.x, a.inv_heads, gkv);
-    t.gkv = (int)gkv;
-    if ((int)i < a.full) {
-      t.b = seq_of<16>(a, (int)i, 0, a.n_seqs);  // (sequences without a full task share their successor's number)
-      part = (int)i - (a.cu[t.b].task >> 16);
-    } else {
-      const int r = (int)i - a.full;
-      t.b = a.rest[r >> 2] >> (8 * (r & 3)) & 255;
-      part = (a.cu[t.b + 1].task >> 16) - (a.cu[t.b].task >> 16);
-    }
-    t.x = (a.cu[t.b].task & 0xffff) + part;
-  }
-  t.B = a.cu[t.b + 1].slot - a.cu[t.b].slot;
-  t.s0 = part * a.chunk;
-  t.s1 = min(t.B, t.s0 + a.chunk);
-  return t;
-}
 
 template <int D, int GP, bool ORDERED>
 __global__ __launch_bounds__(kDThreads) void decode_partial_kernel(DecodeArgs a) {
@@ -531,26 +466,6 @@ static int decode_waves(const Shape &sh, int chunk) {
   const int most = chunk < sh.maxB ? chunk : sh.maxB;
   if (wgs >= 1024 && sh.SB <= 64LL * sh.batch && most <= 8 * 2 * kMRows) return 2;
   return wgs >= 384 && sh.SB <= 256LL * sh.batch && most <= 8 * 4 * kMRows ? 4 : kMWaves;
-}
-
-// What decode_task<true> reads of the order.  (Only where the order counts: the smallest calls are bound by host time.)
-static void order_tasks(DecodeArgs &a, const int *budgets, int units) {
-  int n_rest = 0, rest[kDecodeSeqs];  // slots << 8 | sequence
-  a.full = 0;
-  for (int i = 0; i < a.n_seqs; ++i) {
-    a.cu[i].task |= a.full << 16;
-    a.full += budgets[i] / a.chunk;
-    if (budgets[i] % a.chunk) rest[n_rest++] = budgets[i] % a.chunk << 8 | i;
-  }
-  a.cu[a.n_seqs].task |= a.full << 16;
-  std::sort(rest, rest + n_rest, [](int x, int y) { return x > y; });
-  std::memset(a.rest, 0, sizeof(a.rest));
-  for (int i = 0; i < n_rest; ++i) a.rest[i >> 2] |= (rest[i] & 255) << (8 * (i & 3));
-  const int last = (kDecodeTail + a.tasks - 1) / a.tasks;
-  a.mixed = units > last ? units - last : 0;
-  a.inv_tasks = 0xffffffffu / (unsigned)a.tasks;
-  a.inv_last = 0xffffffffu / (unsigned)(units > last ? last : units);
-  a.inv_heads = 0xffffffffu / (unsigned)a.Hkv;
 }
 
 hipError_t launch_decode_attention(const Shape &sh, const int *budgets, DecodeArgs a, hipStream_t stream) {

@@ -128,6 +128,7 @@ struct DecodeArgs {
   // of a sequence shares a line, for a small batch that of the whole search (16 units x 7 sequences 6.8 -> 6.5 us).
   struct Seq { int slot, task; };
   alignas(64) Seq cu[kDecodeSeqs + 1];
+  __host__ __device__ int rows(int b) const { return cu[b + 1].slot - cu[b].slot; }
 };
 static_assert(offsetof(DecodeArgs, cu) % 64 == 0 && 8 * sizeof(DecodeArgs::Seq) <= 64, "seven sequences and the end in one line");
 hipError_t launch_decode_attention(const Shape &sh, const int *budgets, DecodeArgs a, hipStream_t stream);
@@ -218,11 +219,10 @@ struct ScoreArgs {
   const float *slopes; // [Hq] or NULL
 };
 
-// one step of attention over a cache with head room (cache_attention.hip)
-constexpr int kCacheAttnSeqs = 64;        // sequences per launch
+// one step of attention over a cache with head room (cache_attention.hip); the sequences of a launch ride in its arguments, tasks and order as in DecodeArgs
 constexpr int kCacheAttnLeastPart = 128;  // rows of a part (workgroup) at the least, where a sequence is cut
 constexpr int kCacheAttnMostParts = 64;   // parts of a sequence
-constexpr int kCacheAttnTasks = 1024;     // workgroups that sequences are cut for: at most this many over the (layer, kv head) units and one a sequence
+constexpr int kCacheAttnTasks = 4096;     // sequences are cut into at most this many workgroups more than there are (layer, kv head) units x sequences
 enum RowKind { kRowF32, kRowBF16, kRowFp8 };
 struct CacheAttnArgs {
   const void *q;                // [Lyr][Hq][batch][d]
@@ -234,11 +234,16 @@ struct CacheAttnArgs {
   const int *row_pos;           // [Lyr][Hkv][SB] or NULL
   ScoreArgs score;
   int Hq, Hkv, G, NB, SB, batch;
-  int chunk;                    // rows of a task
+  int chunk, waves;             // rows of a task; waves of a workgroup
   int b0, n_seqs, tasks, g0;    // sequences b0 .. b0 + n_seqs - 1 are in this launch, cut into tasks; first query head inside its kv group
-  struct Seq { int task, len, row, block, merged, slot, q_pos, pad; };
-  alignas(64) Seq seq[kCacheAttnSeqs + 1];
+  int full, mixed;
+  unsigned inv_tasks, inv_last, inv_heads;
+  int rest[kDecodeSeqs / 4];
+  struct Seq { int task, len, row, block, merged, slot, q_pos, pad; };  // task as in DecodeArgs; valid rows, first row, first scale; merged rows, the first one's place in row_pos
+  alignas(64) Seq cu[kDecodeSeqs + 1];
+  __host__ __device__ int rows(int b) const { return cu[b].len; }
 };
+static_assert(sizeof(CacheAttnArgs) <= 4096, "kernel arguments");
 struct CacheAttnCall {
   const int *cu_capacity, *lengths, *budgets, *q_pos;
   int n_layers, d;
