@@ -359,19 +359,29 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
   }
 }
 
-// out[l][h][b] of the sequences that several workgroups have worked on, from their partial states in row order
+// out[l][h][b] of the sequences that several workgroups have worked on.  Lane i weighs part i (there are 64 at most); then the parts are added up in row order, eight
+// loads at a time (one dependent fold after the other took 0.25 us a part).
 template <bool QBF16, int D>
 __global__ __launch_bounds__(D) void cache_attention_combine_kernel(CacheAttnArgs a) {
+  static_assert(kCacheAttnMostParts <= 64, "a lane for every part");
   const int b = blockIdx.x;
-  const int x0 = a.cu[b].task & 0xffff, x1 = a.cu[b + 1].task & 0xffff;
-  if (x1 - x0 < 2) return;
+  const int x0 = a.cu[b].task & 0xffff, n = (a.cu[b + 1].task & 0xffff) - x0;
+  if (n < 2) return;
   const long long head = (long long)blockIdx.z * a.Hq + blockIdx.y;
-  const int ci = threadIdx.x;
+  const int ci = threadIdx.x, lane = threadIdx.x & 63;
   const float *part = a.part + (head * a.tasks + x0) * (D + 2);
-  float mm = part[D], zz = part[D + 1], av = part[ci];
-  for (int sp = 1; sp < x1 - x0; ++sp) {
-    const float *p2 = part + (long long)sp * (D + 2);
-    fold_state(mm, zz, &av, 1, p2[D], p2[D + 1], &p2[ci]);
+  const float m = lane < n ? part[lane * (D + 2) + D] : -INFINITY, z = lane < n ? part[lane * (D + 2) + D + 1] : 0.f;
+  float M = m;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  const float w = fast_exp2(m - M), zz = wave_sum(z * w);  // (M is finite: no part's maximum is below the lowest float)
+  float av = 0.f;
+  for (int i = 0; i < n; i += 8) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = part[min(i + k, n - 1) * (D + 2) + ci];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) av = i + k < n ? fmaf(v[k], __shfl(w, i + k, 64), av) : av;
   }
   const float o = av / zz;
   const long long at = (head * a.batch + a.b0 + b) * D + ci;
