@@ -100,11 +100,12 @@ __global__ __launch_bounds__(kQuantWaves * 64) void cache_dequantize_kernel(Quan
   }
 }
 
-// grid (sequences of the launch, 2 x kv heads, layers), a wave each: the new row of K or of V
-template <bool BF16, int D, int N>
-__global__ __launch_bounds__(64) void cache_append_quantized_kernel(AppendQuantArgs<N> a) {
+// grid (sequences of the launch, WAVES of them a workgroup; 2 x kv heads; layers): a wave places the new row of K or of V
+template <bool BF16, int D, int N, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void cache_append_quantized_kernel(AppendQuantArgs<N> a, int n) {
   constexpr int EPL = D / 64;  // elements of the row in a lane
-  const int b = blockIdx.x, tensor = blockIdx.y & 1, g = blockIdx.y >> 1, l = blockIdx.z, lane = threadIdx.x;
+  const int b = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tensor = blockIdx.y & 1, g = blockIdx.y >> 1, l = blockIdx.z, lane = threadIdx.x & 63;
+  if (b >= n) return;
   const long long unit = (long long)l * (gridDim.y >> 1) + g, at = (unit * a.batch + b) * D + lane * EPL;
   const unsigned where = a.where[b];
   const int inside = (int)(where % kQuantRows), row = a.row[b];
@@ -177,7 +178,9 @@ hipError_t launch_append_quantized_t(const AppendQuantCall &c, int b0, int n, hi
     block += (c.cu_capacity[b + 1] - c.cu_capacity[b] + kQuantRows - 1) / kQuantRows;
   }
   ProfScope ps(stream, KID_CACHE_APPEND_QUANTIZED);
-  cache_append_quantized_kernel<BF16, D, N><<<dim3(n, 2 * c.Hkv, c.n_layers), 64, 0, stream>>>(a);
+  // (four rows a workgroup where there are many sequences, us: 64 x 256 units 9.5 -> 8.0)
+  constexpr int kWaves = N > kAppendSeqsSmall ? 4 : 1;
+  cache_append_quantized_kernel<BF16, D, N, kWaves><<<dim3((n + kWaves - 1) / kWaves, 2 * c.Hkv, c.n_layers), kWaves * 64, 0, stream>>>(a, n);
   return hipGetLastError();
 }
 
