@@ -953,6 +953,33 @@ flowmm_status quantize_call(const flowmm_params *p, const int32_t *cu_capacity, 
   return FLOWMM_OK;
 }
 
+// Waves that share the query rows of the prompt's attention and split the keys, `items` being the groups of 32 rows (all heads, layers): one workgroup of eight waves has a
+// compute unit to itself.  Causal prompts end with short rows that fill gaps, so that the split is worth it up to twice the compute units (bf16, 128 channels, us in
+// one / two / four: 704 items of 675 tokens 25.8 / 17.3 / 18.0, 1216 of 1200 38 / 25 / 34, 2016 of 2000 58 / 43 / 62, 3008 of 3000 90 / 91 / 115; fp32, whose rounds
+// cost what they compute, 1064 of 1200 345 / 188 / 148, 2632 of 3000 846 / 690 / 777).  Rows that nearly all see as much (a prefix or a picture of most of the prompt)
+// take as many rounds as there are: 704 items of 675 tokens, 576 of them a picture, 34.6 / 25.5 / 31.0.
+int prompt_key_split(const flowmm_params *p, const int32_t *prefix, int image_spans, const Shape &sh, long long items) {
+  if (items > 512 && items < 2048 && (prefix || image_spans)) {
+    long long sum = 0, n = 0, most = 0;
+    for (int b = 0; b < sh.batch; ++b) {
+      const int L = p->cu_seqlens[b + 1] - p->cu_seqlens[b];
+      int j = p->cu_spans[b];
+      for (int last = std::min(kPromptRows, L) - 1;; last = std::min(last + kPromptRows, L - 1)) {
+        int reach = prefix && last < prefix[b] ? std::max(last, prefix[b] - 1) : last;
+        while (p->spans[j].end <= last) ++j;
+        if (image_spans && p->spans[j].modality == FLOWMM_IMAGE) reach = std::max(reach, p->spans[j].end - 1);
+        sum += reach + 1;
+        most = std::max(most, (long long)reach + 1);
+        ++n;
+        if (last == L - 1) break;
+      }
+    }
+    if (4 * sum >= 3 * most * n) return items <= 1024 ? 2 : 1;
+  }
+  if (!sh.bf16) return items >= 14 * 256 ? 1 : items >= 6 * 256 ? 2 : 4;
+  return items >= 8 * 256 ? 1 : items >= 4 * 256 ? 2 : 4;
+}
+
 // what the two cache attentions have in common; a.K_c .. and the strides are set
 flowmm_status cache_attention_call(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths, const flowmm_scoring *scoring, const void *q,
                                    void *out, void *workspace, size_t workspace_bytes, CacheAttnArgs &a, RowKind rows, void *stream) {
@@ -1111,7 +1138,7 @@ FLOWMM_API flowmm_status flowmm_prompt_attention(const flowmm_params *p, const f
   long long items = 0;
   for (int b = 0; b < sh.batch; ++b) items += (long long)key_tiles(p, b, kPromptRows) * sh.G;
   const long long waves = items * sh.n_layers * sh.Hkv;
-  a.ksplit = waves >= 8 * 256 ? 1 : waves >= 4 * 256 ? 2 : 4;
+  a.ksplit = prompt_key_split(p, prefix, a.image_spans, sh, waves);
   std::vector<int32_t> words((size_t)PW_HEADER + (size_t)sh.batch * PS_WORDS, 0);
   words[PW_BATCH] = sh.batch;
   words[PW_SPANS] = (int32_t)words.size();

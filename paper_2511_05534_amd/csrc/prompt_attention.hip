@@ -49,20 +49,30 @@ struct ValueTile {
   }
 };
 
-// the last key that row q of the sequence sees
-__device__ __forceinline__ int reach_of(const PromptArgs &a, ScalarInts meta, const int L, const int prefix, const int span0, const int n_spans, int q) {
-  int r = q < prefix ? prefix - 1 : q;
-  if (a.image_spans) {
-    // the span of q: the first whose end is behind it
-    const ScalarInts spans = meta + meta[PW_SPANS] + 2 * span0;
-    int lo = 0, hi = n_spans - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (spans[2 * mid] > q) hi = mid; else lo = mid + 1;
-    }
-    if (spans[2 * lo + 1]) r = max(r, spans[2 * lo] - 1);
+// The first of a sequence's spans (PromptWord) that ends behind row q, and the last key that row q, or this lane's of the rows p0 .. p0 + 31, sees.  All by scalar loads:
+// a search of every lane's own was three dependent trips to memory at a workgroup's start.
+struct PromptSeq { int L, prefix, n_spans; ScalarInts spans; };
+__device__ __forceinline__ int span_of(const PromptSeq &s, int q) {
+  int lo = 0, hi = s.n_spans - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (s.spans[2 * mid] > q) hi = mid; else lo = mid + 1;
   }
-  return min(r, L - 1);
+  return lo;
+}
+__device__ __forceinline__ int reach_of_rows(const PromptSeq &s, bool image_spans, int p0, int rows, int q) {
+  int r = q < s.prefix ? max(q, s.prefix - 1) : q;
+  if (image_spans) {
+    int j = span_of(s, p0), begin = p0;
+    for (;;) {
+      const int end = s.spans[2 * j];
+      if (s.spans[2 * j + 1] && q >= begin && q < end) r = max(r, end - 1);
+      if (end >= p0 + rows || j + 1 >= s.n_spans) break;
+      begin = end;
+      ++j;
+    }
+  }
+  return r;
 }
 
 // A wave's share of the call: the rows p0 .. p0 + 31 of query head h, and the keys that they see.
@@ -86,8 +96,8 @@ __device__ __forceinline__ PromptWave prompt_wave(const PromptArgs &a, ScalarInt
     if (meta[PW_HEADER + mid * PS_WORDS + PS_WG] <= x) b = lo = mid; else hi = mid;
   }
   const ScalarInts rec = meta + PW_HEADER + b * PS_WORDS;
-  const int prefix = rec[PS_PREFIX], span0 = rec[PS_SPAN], n_spans = rec[PS_N_SPANS];
-  w.L = rec[PS_L];
+  const PromptSeq seq = {rec[PS_L], rec[PS_PREFIX], rec[PS_N_SPANS], meta + meta[PW_SPANS] + 2 * rec[PS_SPAN]};
+  w.L = seq.L;
   w.tok = rec[PS_TOK];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = threadIdx.x & 31;
   // item i of the sequence: head i % G of the kv group, query rows [32 * (i / G), + 32)
@@ -98,8 +108,8 @@ __device__ __forceinline__ PromptWave prompt_wave(const PromptArgs &a, ScalarInt
   w.h = w.gkv * a.G + (item - pb * a.G);
   w.p0 = pb * kPromptRows;
   const int wg_row = min((min(first + kItems, items) - 1) / a.G * kPromptRows + kPromptRows, w.L) - 1;
-  w.wg_last = __builtin_amdgcn_readfirstlane(reach_of(a, meta, w.L, prefix, span0, n_spans, wg_row));
-  w.limit = reach_of(a, meta, w.L, prefix, span0, n_spans, min(w.p0 + n, w.L - 1));
+  w.wg_last = __builtin_amdgcn_readfirstlane(reach_of_rows(seq, a.image_spans, wg_row, 1, wg_row));
+  w.limit = reach_of_rows(seq, a.image_spans, w.p0, kPromptRows, min(w.p0 + n, w.L - 1));
   w.first = __builtin_amdgcn_readfirstlane(w.limit);
   w.last = mine < items ? __builtin_amdgcn_readlane(w.limit, 31) : -1;
   return w;
