@@ -4,8 +4,8 @@
 
 namespace flowmm {
 
-// log2(e) * cap * tanh(scale * x / cap).  tanh u = 1 - 2 / (1 + e^(2u)): exact at both ends, and off by 2^-23 of the cap near 0, where the
-// logits of an fp32 call deserve better: there the power series, whose first term left out is below 2^-26 of it for |u| < 1/4.
+// log2(e) * cap * tanh(scale * x / cap).  tanh u = 1 - 2 / (1 + e^(2u)): exact at both ends, and off by 2^-22 of the cap near 0, where the
+// logits of an fp32 call, or of one with a large cap, deserve better: there (FINE) the power series, whose first term left out is below 2^-26 of it for |u| < 1/4.
 template <bool FINE>
 __device__ __forceinline__ float capped(const ScoreArgs &s, float x) {
   const float u = x * s.cap_in;

@@ -192,8 +192,13 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
     for (int u = 0; u < SUBS; ++u) {
       if constexpr (R == kRowFp8) p[u] *= kscale;
       if (a.score.cap > 0.f) {
+        if (!QBF16 || a.score.fine) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[u][i] = capped<!QBF16>(a.score, p[u][i]);
+          for (int i = 0; i < 4; ++i) p[u][i] = capped<true>(a.score, p[u][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[u][i] = capped<false>(a.score, p[u][i]);
+        }
       } else {
         p[u] *= a.score.cl;
       }

@@ -854,13 +854,14 @@ namespace {
 // ---- attention with scored and masked logits; the cache in 8 bits ---------------------------------------
 flowmm_status check_scoring(const flowmm_scoring *scoring, float scale, ScoreArgs &out) {
   constexpr float kLog2e = 1.4426950408889634f;
-  out = ScoreArgs{scale * kLog2e, 0.f, 0.f, nullptr};
+  out = ScoreArgs{scale * kLog2e, 0.f, 0.f, nullptr, 0};
   if (!scoring) return FLOWMM_OK;
   const float cap = scoring->cap;
   if (!(cap >= 0.f) || !std::isfinite(cap * kLog2e)) return fail(FLOWMM_EINVAL, "cap must be finite and >= 0");
   if (cap > 0.f) {
     out.cap = cap * kLog2e;
     out.cap_in = scale / cap;
+    out.fine = cap > 512.f;
     if (!std::isfinite(out.cap_in)) return fail(FLOWMM_EINVAL, "cap is too small for the scale");
   }
   if (reinterpret_cast<uintptr_t>(scoring->slopes) & 3) return fail(FLOWMM_EINVAL, "slopes is not 4-byte aligned");

@@ -217,6 +217,7 @@ struct ScoreArgs {
   float cl;            // scale * log2(e)
   float cap, cap_in;   // cap * log2(e), or 0: not capped; scale / cap
   const float *slopes; // [Hq] or NULL
+  int fine;            // the cap is so large that small logits need more than 2^-22 of it also for bf16 results
 };
 
 // one step of attention over a cache with head room (cache_attention.hip); the sequences of a launch ride in its arguments, tasks and order as in DecodeArgs

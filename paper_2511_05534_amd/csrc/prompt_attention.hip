@@ -159,27 +159,26 @@ __device__ __forceinline__ void store_rows(const PromptArgs &a, const PromptWave
   }
 }
 
-// log2-domain scores of the products s[first .. first + N - 1] of row q with the keys key + acc_row(i, 0) (key: of this lane's half)
-template <bool SCORED, int N, bool FINE = false>
-__device__ __forceinline__ void score(const PromptArgs &a, f32x16_t &s, int first, float slope, int key, int q) {
+// log2-domain scores of the products of row q with the keys key + acc_row(i, 0) (key: of this lane's half)
+template <bool SCORED, bool FINE>
+__device__ __forceinline__ void score(const PromptArgs &a, f32x16_t &s, float slope, int key, int q) {
 #pragma clang fp contract(off)
   if (SCORED && a.score.cap > 0.f) {
+    if (FINE || a.score.fine) {
 #pragma unroll
-    for (int i = first; i < first + N; ++i) s[i] = capped<FINE>(a.score, s[i]);
+      for (int i = 0; i < 16; ++i) s[i] = capped<true>(a.score, s[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = capped<false>(a.score, s[i]);
+    }
   } else {
 #pragma unroll
-    for (int i = first; i < first + N; ++i) s[i] *= a.score.cl;
+    for (int i = 0; i < 16; ++i) s[i] *= a.score.cl;
   }
   if (SCORED && a.score.slopes) {
 #pragma unroll
-    for (int i = first; i < first + N; ++i) s[i] = fmaf(-slope, fabsf((float)(key - q + acc_row(i, 0))), s[i]);
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(-slope, fabsf((float)(key - q + acc_row(i, 0))), s[i]);
   }
-}
-
-// exp2(s - m), s a rounded score.  (Not a fused multiply-add of the product: what that keeps of a product's rounding is 2^-24 of it, and logits may be 1e30.)
-__device__ __forceinline__ float weight(float s, float m) {
-#pragma clang fp contract(off)
-  return fast_exp2(s - m);
 }
 
 // (an LDS address is 32 bits wide; the cast goes through uintptr_t for the host's pass over this file)
@@ -313,27 +312,40 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
         for (int i = u ? 0 : 2; i < 16; i += 2) x = fmaxf(fmaxf(x, s[u][i]), s[u][i + 1]);
       return x;
     };
-    // Whole blocks: weights exp2(fma(product, scale, -maximum)), which keeps what the maximum's own rounding lost, 2^-24 of it: nothing where scores are
-    // within 2^24, an overflow at 1e30.  Larger ones (or NaN) are rounded first, as everywhere else.
-    float mul = 1.f, tm = 0.f;
-    bool fused = !MASKED && !SCORED;
+    // Weights are exp2(score - maximum), taken as exp2(fma(s, mul, add - maximum)) with whatever is left in s: the product, where whole blocks are neither capped nor
+    // biased; -1 / (1 + e^(2 u)), where they are capped only (the cap's own rounding is larger); the score.  A product's fused multiply-add keeps what the maximum's
+    // rounding lost, 2^-24 of it: nothing where scores are within 2^24, an overflow at 1e30.  Larger ones (or NaN) are rounded first.
+    float mul = 1.f, add = 0.f, tm = 0.f;
+    bool ready = false;
     if constexpr (!MASKED && !SCORED) {
       tm = most();
-      fused = !__any(!(fabsf(tm) * a.score.cl < 0x1p24f));
-      if (fused) { mul = a.score.cl; tm *= mul; }
+      ready = !__any(!(fabsf(tm) * a.score.cl < 0x1p24f));
+      if (ready) mul = a.score.cl;
     }
-    if (!fused) {
+    if (!ready) {
+      if (SCORED && BF16 && a.score.cap > 0.f && !a.score.slopes && !a.score.fine) {
+        mul = 2.f * a.score.cap;
+        add = a.score.cap;
+        const float k = a.score.cap_in * 2.8853900817779268f;
 #pragma unroll
-    for (int u = 0; u < NB; ++u) {
-      score<SCORED, 16, !BF16>(a, s[u], 0, slope, key0 + 32 * u * KS + 4 * half, p0 + n);
-      if constexpr (MASKED) {
-        const int last = limit - key0 - 32 * u * KS - 4 * half;
+        for (int u = 0; u < NB; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][i] = acc_row(i, 0) <= last ? s[u][i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) s[u][i] = __builtin_amdgcn_rcpf(-1.f - fast_exp2(s[u][i] * k));
+      } else {
+#pragma unroll
+        for (int u = 0; u < NB; ++u) score<SCORED, !BF16>(a, s[u], slope, key0 + 32 * u * KS + 4 * half, p0 + n);
       }
+      if constexpr (MASKED) {
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+          const int last = limit - key0 - 32 * u * KS - 4 * half;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[u][i] = acc_row(i, 0) <= last ? s[u][i] : -INFINITY;
+        }
+      }
+      tm = most();
     }
-    tm = most();
-    }
+    tm = fmaf(tm, mul, add);
     if (__any(tm > m + kLazy)) {
       const float M = fmaxf(m, fmaxf(tm, __shfl_xor(tm, 32, 64))), f = fast_exp2(m - M);
       z *= f;
@@ -343,13 +355,14 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
         for (int i = 0; i < 16; ++i) o[c][i] *= f;
       m = M;
     }
+    const float base = add - m;
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
       float za = 0.f, zb = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        s[u][i] = !MASKED && !SCORED ? fast_exp2(fmaf(s[u][i], mul, -m)) : weight(s[u][i], m);
-        s[u][i + 1] = !MASKED && !SCORED ? fast_exp2(fmaf(s[u][i + 1], mul, -m)) : weight(s[u][i + 1], m);
+        s[u][i] = fast_exp2(fmaf(s[u][i], mul, base));
+        s[u][i + 1] = fast_exp2(fmaf(s[u][i + 1], mul, base));
         za += s[u][i];
         zb += s[u][i + 1];
       }

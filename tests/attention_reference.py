@@ -3,7 +3,8 @@
 Bounds (relative to the weighted magnitudes M = sum_j p_j |v_j| of an output, beside the rounding of the result itself, half a step of its
 type): the weights p = exp(x - m) carry the absolute error of x twice (in p and in the sum).  x is a sum of d products, each partial sum
 rounded to fp32 (and in cases of fp32 queries beside 8-bit rows a product short of 2^-24 of itself): (d + 4) * 2^-24 of scale * sum |q k|.
-A cap adds 2^-20 of itself (one reciprocal and one exponential of 2^-22 each), a bias 2^-22 of its size, exp2 2^-22, and the sum over n rows
+A cap adds 2^-20 of itself (one reciprocal and one exponential of 2^-22 each; of fp32 calls and caps above 512, where |x| is below a quarter of
+the cap, 2^-21 of x: a power series), a bias 2^-22 of its size, exp2 2^-22, and the sum over n rows
 n * 2^-24 (its partial sums).  Weights in two bf16 terms are short of 2^-15; in one, of half a step: 2^-8."""
 import math
 
@@ -53,8 +54,9 @@ def attend(q, k, v, scale, cap, slope, distance, hidden, out_dtype, weight_error
     x = q @ k.T * scale
     err = (d + 4) * 2.0 ** -24 * scale * (q.abs() @ k.abs().T)
     if cap > 0:
+        near = x.abs() < cap / 4 if cap > 512 or out_dtype == torch.float32 else torch.zeros_like(x, dtype=torch.bool)
+        err = err + torch.where(near, x.abs() * 2.0 ** -21, cap * 2.0 ** -20)
         x = cap * torch.tanh(x / cap)
-        err = err + cap * 2.0 ** -20
     if slope is not None:
         x = x - slope * distance
         err = err + slope * distance * 2.0 ** -22

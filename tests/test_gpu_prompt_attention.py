@@ -114,6 +114,15 @@ def test_scores_and_masks(dtype, cap, slopes, prefix, image_spans):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap, slopes", [(0.5, False), (512.0, False), (513.0, False), (1e5, False), (1e5, True), (1e30, False)])
+def test_caps_of_any_size(dtype, cap, slopes):
+    """Caps far above the logits leave them as they are, small ones flatten them."""
+    a = Prompt(dtype, 1, 4, 2, 64, [130], cap=cap, slopes=slopes, seed=18)
+    a.run()
+    a.check(f"{dtype} cap {cap}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_spans_and_sequences(dtype):
     """More words of description than a kernel's arguments hold."""
     lens = [30 + b for b in range(40)]

@@ -307,6 +307,15 @@ def test_attention_scores(rows, dtype, cap, slopes, positions):
 
 
 @pytest.mark.parametrize("rows, dtype", KINDS)
+@pytest.mark.parametrize("cap", [0.5, 512.0, 513.0, 1e5, 1e30])
+def test_attention_caps_of_any_size(rows, dtype, cap):
+    """Caps far above the logits leave them as they are, small ones flatten them."""
+    a = Attention(rows, dtype, 1, 4, 2, 64, [70, 33], cap=cap, seed=14)
+    a.run()
+    a.check(f"{rows} {dtype} cap {cap}")
+
+
+@pytest.mark.parametrize("rows, dtype", KINDS)
 def test_attention_long_sequences_in_parts(rows, dtype):
     """One unit and a long sequence: many workgroups and the fold; beside it a short one and an empty one."""
     a = Attention(rows, dtype, 1, 4, 1, 128, [9001, 3, 0], cap=30.0, slopes=True, seed=6)
