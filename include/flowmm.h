@@ -259,10 +259,12 @@ typedef struct {
  *   out[l][h][t] = sum_j softmax_j(x_tj) V[l][kv(h)][j]
  * over the keys j that token t of its sequence sees: all up to itself, and where the scoring says so
  * all of the prefix (t in it) or of its image span.  The sequences of the batch do not see each
- * other.  K, V through p's k strides; Q_full and out [Lyr][Hq][T][d] through the three
- * strides given (as for flowmm_flow_exact); out must not overlap the inputs.  The weights of bf16 calls are
- * rounded to bf16 for the product with V (their sum is not), the sums are fp32.  p, workspace (size from flowmm_plan_sizes),
- * stream and errors as for flowmm_plan; window, budgets, tau and theta are validated but not used. */
+ * other.  K, V through p's k strides; Q_full and out [Lyr][Hq][T][d] through the three strides given
+ * (elements; head_dim contiguous; 32 consecutive tokens of a head must lie within 4 GiB,
+ * FLOWMM_EUNSUPPORTED otherwise); out must not overlap the inputs.  What a token does not see does not
+ * reach it, infinities and NaN included.  The weights of bf16 calls are rounded to bf16 for the product with V (their
+ * sum is not), all sums are fp32.  p, workspace (size from flowmm_plan_sizes), stream and errors as for
+ * flowmm_plan; window, budgets, tau and theta are validated but not used. */
 flowmm_status flowmm_prompt_attention(const flowmm_params *p, const flowmm_scoring *scoring, const void *K, const void *V,
                                       const void *Q_full, int64_t qf_stride_layer, int64_t qf_stride_head,
                                       int64_t qf_stride_token, void *out, void *workspace, size_t workspace_bytes,

@@ -257,8 +257,8 @@ class Scoring:
     integers per sequence."""
 
     def __init__(self, cap: float = 0.0, slopes: int = 0, prefix=None, image_spans: bool = False, row_pos: int = 0, q_pos=None):
-        self._prefix, prefix_p = (None, None) if prefix is None else _i32_array(prefix)
-        self._q_pos, q_pos_p = (None, None) if q_pos is None else _i32_array(q_pos)
+        self._prefix, prefix_p = (None, None) if prefix is None else _i32_array(np.ascontiguousarray(prefix, dtype=np.int32))
+        self._q_pos, q_pos_p = (None, None) if q_pos is None else _i32_array(np.ascontiguousarray(q_pos, dtype=np.int32))
         self.c = flowmm_scoring(float(cap), slopes or None, prefix_p, int(bool(image_spans)), row_pos or None, q_pos_p)
 
     def address(self, batch: int) -> int:
@@ -275,7 +275,7 @@ def _scoring(scoring: Scoring | None, params: Params):
 
 def flowmm_cache_sizes(params: Params, cu_capacity) -> Tuple[int, int, int]:
     """Bytes of a cache's codes and of its scales (K's, or V's) in 8 bits, and of the cache attentions' workspace."""
-    cap, cap_p = _i32_array(cu_capacity)
+    cap, cap_p = _i32_array(np.ascontiguousarray(cu_capacity, dtype=np.int32))
     if cap.size < params.batch + 1:
         raise ValueError(f"cu_capacity has {cap.size} entries, {params.batch + 1} expected")
     n = [C.c_size_t(0) for _ in range(3)]

@@ -1117,6 +1117,8 @@ FLOWMM_API flowmm_status flowmm_prompt_attention(const flowmm_params *p, const f
   for (int i = 0; i < 3; ++i)
     if (strides[i] < 0 || strides[i] % epc != 0) return fail(FLOWMM_EINVAL, "strides must be non-negative multiples of 16 bytes (%d elements)", epc);
   if (qf_stride_token < sh.d) return fail(FLOWMM_EINVAL, "token strides must be at least head_dim");
+  if ((sh.n_layers > 1 && qf_stride_layer == 0) || (sh.Hq > 1 && qf_stride_head == 0))
+    return fail(FLOWMM_EINVAL, "strides of 0 would write the outputs of several heads or layers to one place");
   // a wave's query rows are addressed with 32-bit byte offsets from its first one
   if ((31 * qf_stride_token + sh.d) * es >= (int64_t)1 << 32) return fail(FLOWMM_EUNSUPPORTED, "32 query rows span 4 GiB or more");
   PromptArgs a;

@@ -137,7 +137,21 @@ def test_prompt_attention():
         refused(call(**kw), word)
     for kw, word in SCORING:
         refused(call(scoring=fb.Scoring(**kw)), word)
-    refused(call(qs=(0, 0, 1 << 27)), "4 GiB", fb.FLOWMM_EUNSUPPORTED)
+    refused(call(qs=(qs[0], 0, 128)), "one place")
+    refused(call(qs=(0, qs[1], 128)), "one place")
+    refused(call(qs=(128, 128, 1 << 27)), "4 GiB", fb.FLOWMM_EUNSUPPORTED)
     refused(call(n=ws - 1), "workspace", fb.FLOWMM_EWORKSPACE)
     with pytest.raises(ValueError, match="prefix"):
         call(scoring=fb.Scoring(prefix=[1]))()
+
+
+def test_integer_arrays_of_any_form():
+    """Strided and wider arrays are read as what they hold."""
+    import numpy as np
+    p = params()
+    wide = np.array([0, 7, 40, 7, 90])[::2]
+    assert fb.flowmm_cache_sizes(p, wide) == fb.flowmm_cache_sizes(p, CAP)
+    assert fb.flowmm_cache_sizes(p, wide.astype(np.int32)[::1]) == fb.flowmm_cache_sizes(p, np.array([0, 9, 40, 9, 90], np.int32)[::2])
+    for values in ([3, 4], (3, 4), np.array([3, 4]), np.array([3, 9, 4, 9], np.int32)[::2]):
+        s = fb.Scoring(prefix=values, q_pos=values, row_pos=good)
+        assert [s.c.prefix[i] for i in range(2)] == [3, 4] and [s.c.q_pos[i] for i in range(2)] == [3, 4]

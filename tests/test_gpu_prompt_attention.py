@@ -146,6 +146,45 @@ def test_long_prompt(dtype, units):
     assert torch.equal(a.out, first)
 
 
+@pytest.mark.parametrize("dtype, L, cap, slopes", [("bf16", 2100, 0.0, False), ("bf16", 2100, 15.0, False), ("bf16", 2090, 0.0, True), ("bf16", 2100, 600.0, True), ("f32", 3700, 0.0, False)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_rows_than_the_compute_units_take_at_once(dtype, L, cap, slopes, d):
+    """Every wave has rows of its own and whole blocks of keys two at a time."""
+    a = Prompt(dtype, 1, 32, 8, d, [L], cap=cap, slopes=slopes, seed=19)
+    a.run()
+    a.check(f"{dtype} {L} {d} cap {cap} slopes {slopes}", heads=[0, 31])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L, hq", [(700, 24), (1100, 32)])
+def test_pictures_of_most_of_the_prompt(dtype, L, hq):
+    """Rows that nearly all see as much: another split of the keys."""
+    a = Prompt(dtype, 1, hq, hq, 64, [L], spans=[[(0, 20, 0), (20, L - 30, 1), (L - 30, L, 0)]], image_spans=True, seed=20)
+    a.run()
+    a.check(f"{dtype} {L} {hq}", heads=[0, hq - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("power", [0, 20, 60])
+def test_scores_of_any_size(dtype, power):
+    """Logits 2^power apart, the largest beyond 2^24 or 1e18: the visible keys of the largest one weigh the same, the others nothing."""
+    L = 300
+    a = Prompt(dtype, 1, 2, 1, 64, [L], seed=22)
+    level = torch.randint(-3, 4, (L,), generator=torch.Generator().manual_seed(5)).float()
+    a.Q[:] = 0.0
+    a.Q[..., 0] = 2.0 ** power * 8 * 128  # (scale is an eighth)
+    a.K[:] = 0.0
+    a.K[0, 0, :, 0] = level.to(a.K.dtype)
+    a.upload()
+    a.run()
+    torch.cuda.synchronize()
+    got, V = a.out.cpu().double()[0, 0], a.V[0, 0].double()
+    top = torch.cummax(level, 0).values
+    weight = torch.tril((level[None, :] == top[:, None]).double())
+    want, size = weight @ V / weight.sum(-1, keepdim=True), weight @ V.abs() / weight.sum(-1, keepdim=True)
+    assert ((got - want).abs() <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -14) * size + 1e-30).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strides_and_scale(dtype):
     a = Prompt(dtype, 2, 6, 2, 64, [70, 45], token_major=True, scale=0.21, seed=10)

@@ -329,6 +329,71 @@ def test_attention_long_sequences_in_parts(rows, dtype):
 
 
 @pytest.mark.parametrize("rows, dtype", KINDS)
+@pytest.mark.parametrize("layers, hkv, G, d, lens", [
+    (8, 8, 1, 128, [0, 700, 30, 1500, 0, 90]),    # unequal sequences' order, empty ones in it
+    (16, 16, 1, 64, [0, 600, 5, 300, 33]),        # .. with units whose tasks go one after the other
+    (2, 1, 20, 128, [5000, 1]),                   # more heads than one pass takes, in parts
+    (8, 8, 1, 64, [60, 1, 31, 64, 50]), (16, 16, 1, 64, [100, 3]), (16, 16, 2, 128, [400, 37]),  # fewer waves
+])
+def test_attention_schedules(rows, dtype, layers, hkv, G, d, lens):
+    a = Attention(rows, dtype, layers, hkv * G, hkv, d, lens, slopes=True, merged=[max(1, n // 2) for n in lens], seed=21)
+    a.run()
+    a.check(f"{rows} {dtype} {layers} x {hkv} {lens}")
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """Two calls at once, on caches of their own."""
+    a, b = (Attention("fp8", "bf16", 1, 4, 1, 128, [6000, 10], cap=20.0, seed=s) for s in (30, 31))
+    for x in (a, b):
+        x.run()
+    torch.cuda.synchronize()
+    want = [x.out.clone() for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for x in (a, b):
+        x.out.fill_(0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, st in zip((a, b), streams):
+            x.run(st.cuda_stream)
+    torch.cuda.synchronize()
+    for x, w in zip((a, b), want):
+        assert torch.equal(x.out, w)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_in_a_graph(dtype):
+    """Quantize, append and dequantize captured together: every replay starts from the same rows and ends with the same codes."""
+    layers, hkv, d, lens, caps = 2, 2, 64, [40, 7, 0], [64, 32, 33]
+    cu, cb = sums(caps), sums(blocks_of(caps))
+    p = params(layers, hkv, hkv, d, dtype, caps)
+    K, V = (rows_like_a_cache((layers, hkv, cu[-1], d), DT[dtype], s).to(DEV) for s in (40, 41))
+    k, v = (100 * rows_like_a_cache((layers, hkv, 3, d), DT[dtype], s).to(DEV) for s in (42, 43))
+    cache = fb.QuantizedCache(p, cu, DEV)
+    back = [torch.zeros_like(K) for _ in range(2)]
+
+    def run():
+        st = stream()
+        fb.flowmm_cache_quantize(p, cu, lens, cu, K.data_ptr(), V.data_ptr(), cache, st)
+        fb.flowmm_cache_append_quantized(p, cu, lens, cache, k.data_ptr(), v.data_ptr(), st)
+        fb.flowmm_cache_dequantize(p, cu, [n + 1 for n in lens], cu, cache, back[0].data_ptr(), back[1].data_ptr(), st)
+
+    run()
+    torch.cuda.synchronize()
+    want = [t.view(torch.uint8).clone() for t in (cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales, *back)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        for t in (cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales, *back):
+            t.view(torch.uint8).zero_()
+        torch.randn(1 << 20, device=DEV).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip((cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales, *back), want):
+            assert torch.equal(t.view(torch.uint8), w)
+
+
+@pytest.mark.parametrize("rows, dtype", KINDS)
 def test_attention_of_many_sequences(rows, dtype):
     """More sequences than one launch takes, positions among them."""
     lens = [(7 * b) % 50 for b in range(70)]
