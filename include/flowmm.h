@@ -246,7 +246,7 @@ flowmm_status flowmm_cache_remerge(const flowmm_params *p, const int32_t *cu_cap
  * prefix and image_spans are read by flowmm_prompt_attention, row_pos and q_pos by the two cache
  * attentions (which need both or neither). */
 typedef struct {
-  float cap;              /* finite, >= 0; 0: no cap */
+  float cap;              /* within [0, 2^120], scale / cap as well; 0: no cap */
   const float *slopes;    /* device [Hq], or NULL: no bias */
   const int32_t *prefix;  /* host [batch], 0 <= prefix[b] <= L_b, or NULL: the first prefix[b] tokens of sequence b see each other */
   int32_t image_spans;    /* not 0: an image token sees its whole span */
@@ -277,7 +277,7 @@ flowmm_status flowmm_prompt_attention(const flowmm_params *p, const flowmm_scori
 /* One decode step of attention over a cache with head room: for every layer l, query head h and sequence b
  *   out[l][h][b] = sum_r softmax_r(x_r) V_c[l][kv(h)][cu_capacity[b] + r],   r < lengths[b],
  * q, out [Lyr][Hq][batch][d] contiguous, dtype of the cache.  32 consecutive rows must lie within 4 GiB
- * (FLOWMM_EUNSUPPORTED otherwise).  Rows from lengths[b] on are not read. */
+ * (FLOWMM_EUNSUPPORTED otherwise).  Rows from lengths[b] on are not read; the caller keeps out clear of the cache. */
 flowmm_status flowmm_cache_attention(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
                                      const flowmm_scoring *scoring, const void *q, const void *K_c, const void *V_c,
                                      void *out, void *workspace, size_t workspace_bytes, void *stream);
@@ -302,12 +302,14 @@ flowmm_status flowmm_cache_sizes(const flowmm_params *p, const int32_t *cu_capac
  * necessarily ascending) of K_rows / V_rows, which p's k strides address: the outputs of flowmm_merge with the budgets'
  * prefix sums, or a cache with cu_capacity itself.  A block's scale is the smallest power of two, 2^-120 at the least, that
  * brings its largest finite number within 448; codes are rounded to nearest-even, infinities become
- * +-448, NaN stays NaN.  Rows and scales behind the lengths[b] are left as they were. */
+ * +-448, NaN stays NaN.  Rows and scales behind the lengths[b] are left as they were.  Sequences may share
+ * rows here, but not codes; the caller keeps rows and codes apart. */
 flowmm_status flowmm_cache_quantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
                                     const int32_t *cu_rows, const void *K_rows, const void *V_rows,
                                     const flowmm_quantized_cache *cache, void *stream);
 
-/* The way back, for a re-merge: rows code * scale, rounded to nearest-even in the dtype of p. */
+/* The way back, for a re-merge: rows code * scale, rounded to nearest-even in the dtype of p; here
+ * sequences must not share rows. */
 flowmm_status flowmm_cache_dequantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
                                       const int32_t *cu_rows, const flowmm_quantized_cache *cache, void *K_rows,
                                       void *V_rows, void *stream);

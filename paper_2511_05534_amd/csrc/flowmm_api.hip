@@ -857,12 +857,12 @@ flowmm_status check_scoring(const flowmm_scoring *scoring, float scale, ScoreArg
   out = ScoreArgs{scale * kLog2e, 0.f, 0.f, nullptr, 0};
   if (!scoring) return FLOWMM_OK;
   const float cap = scoring->cap;
-  if (!(cap >= 0.f) || !std::isfinite(cap * kLog2e)) return fail(FLOWMM_EINVAL, "cap must be finite and >= 0");
+  if (!(cap >= 0.f) || cap > 0x1p120f) return fail(FLOWMM_EINVAL, "cap must be within [0, 2^120]");
   if (cap > 0.f) {
     out.cap = cap * kLog2e;
     out.cap_in = scale / cap;
     out.fine = cap > 512.f;
-    if (!std::isfinite(out.cap_in)) return fail(FLOWMM_EINVAL, "cap is too small for the scale");
+    if (!(out.cap_in <= 0x1p120f)) return fail(FLOWMM_EINVAL, "cap is too small for the scale");  // (the kernels multiply either by less than 2^8)
   }
   if (reinterpret_cast<uintptr_t>(scoring->slopes) & 3) return fail(FLOWMM_EINVAL, "slopes is not 4-byte aligned");
   out.slopes = scoring->slopes;
@@ -880,6 +880,7 @@ flowmm_status check_cache(const flowmm_params *p, const int32_t *cu_capacity, co
   if (p->dtype != FLOWMM_F32 && p->dtype != FLOWMM_BF16) return fail(FLOWMM_EINVAL, "dtype must be FLOWMM_F32 or FLOWMM_BF16");
   if (p->head_dim != 64 && p->head_dim != 128) return fail(FLOWMM_EUNSUPPORTED, "head_dim %d is not built (64 and 128 are)", p->head_dim);
   if (p->n_q_heads > 1024 || p->n_layers > 65535) return fail(FLOWMM_EUNSUPPORTED, "more than 1024 query heads or 65535 layers");
+  if (cu_capacity[p->batch] > 0x7fffffff - 65536) return fail(FLOWMM_EUNSUPPORTED, "more than 2^31 - 65537 rows");  // (a step past the last row must be an int)
   if (!lengths) return FLOWMM_OK;
   for (int b = 0; b < p->batch; ++b) {
     const int cap = cu_capacity[b + 1] - cu_capacity[b];
@@ -897,7 +898,12 @@ flowmm_status check_k_strides(const flowmm_params *p) {
   return FLOWMM_OK;
 }
 
-flowmm_status check_quantized(const flowmm_params *p, const flowmm_quantized_cache *c) {
+// rows that a call writes must have places of their own
+bool in_one_place(const flowmm_params *p, int64_t stride_layer, int64_t stride_head) {
+  return (p->n_layers > 1 && stride_layer == 0) || (p->n_kv_heads > 1 && stride_head == 0);
+}
+
+flowmm_status check_quantized(const flowmm_params *p, const flowmm_quantized_cache *c, bool written) {
   if (!c) return fail(FLOWMM_EINVAL, "cache is NULL");
   if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return fail(FLOWMM_EINVAL, "k_codes, v_codes, k_scales and v_scales must not be NULL");
   if (misaligned(c->k_codes) || misaligned(c->v_codes)) return fail(FLOWMM_EINVAL, "k_codes and v_codes must be 16-byte aligned");
@@ -906,6 +912,7 @@ flowmm_status check_quantized(const flowmm_params *p, const flowmm_quantized_cac
   for (int i = 0; i < 3; ++i)
     if (strides[i] < 0 || strides[i] % 16 != 0) return fail(FLOWMM_EINVAL, "the strides of the codes must be non-negative multiples of 16 bytes");
   if (c->stride_token < p->head_dim) return fail(FLOWMM_EINVAL, "the token stride of the codes must be at least head_dim");
+  if (written && in_one_place(p, c->stride_layer, c->stride_head)) return fail(FLOWMM_EINVAL, "strides of 0 would write the codes of several heads or layers to one place");
   return FLOWMM_OK;
 }
 
@@ -916,7 +923,7 @@ long long quant_blocks(const flowmm_params *p, const int32_t *cu_capacity) {
   return n;
 }
 
-// Partial states of the cache attention, at whatever lengths within the capacities (rows_of_task keeps to this).
+// Partial states of the cache attention, at whatever lengths within the capacities (choose_tasks keeps to this).
 size_t cache_attention_bytes(const flowmm_params *p, const int32_t *cu_capacity) {
   const long long units = (long long)p->n_layers * p->n_kv_heads;
   long long parts = 0;
@@ -936,10 +943,18 @@ flowmm_status quantize_call(const flowmm_params *p, const int32_t *cu_capacity, 
   if (!lengths || !cu_rows) return fail(FLOWMM_EINVAL, "lengths and cu_rows must not be NULL");
   for (int b = 0; b < p->batch; ++b)
     if (cu_rows[b] < 0) return fail(FLOWMM_EINVAL, "cu_rows[%d] is negative", b);
-  if ((st = check_k_strides(p)) != FLOWMM_OK || (st = check_quantized(p, cache)) != FLOWMM_OK) return st;
+  if ((st = check_k_strides(p)) != FLOWMM_OK || (st = check_quantized(p, cache, !back)) != FLOWMM_OK) return st;
+  if (back) {
+    if (in_one_place(p, p->k_stride_layer, p->k_stride_head)) return fail(FLOWMM_EINVAL, "strides of 0 would write the rows of several heads or layers to one place");
+    std::vector<std::pair<long long, int>> rows;
+    for (int b = 0; b < p->batch; ++b)
+      if (lengths[b] > 0) rows.push_back({cu_rows[b], lengths[b]});
+    std::sort(rows.begin(), rows.end());
+    for (size_t i = 1; i < rows.size(); ++i)
+      if (rows[i].first < rows[i - 1].first + rows[i - 1].second) return fail(FLOWMM_EINVAL, "cu_rows would write rows of two sequences to one place");
+  }
   if (!K_rows || !V_rows) return fail(FLOWMM_EINVAL, "K_rows and V_rows must not be NULL");
   if (misaligned(K_rows) || misaligned(V_rows)) return fail(FLOWMM_EINVAL, "K_rows and V_rows must be 16-byte aligned");
-  if (p->n_kv_heads > 32767) return fail(FLOWMM_EUNSUPPORTED, "more than 32767 kv heads");
   const int epc = p->dtype == FLOWMM_BF16 ? 8 : 4;
   QuantArgs a;
   a.K_rows = K_rows; a.V_rows = V_rows;
@@ -1056,10 +1071,9 @@ FLOWMM_API flowmm_status flowmm_cache_append_quantized(const flowmm_params *p, c
     const int cap = cu_capacity[b + 1] - cu_capacity[b];
     if (lengths[b] == cap) return fail(FLOWMM_EINVAL, "the cache of sequence %d is full (%d rows): re-merge it before appending", b, cap);
   }
-  if ((st = check_quantized(p, cache)) != FLOWMM_OK) return st;
+  if ((st = check_quantized(p, cache, true)) != FLOWMM_OK) return st;
   if (!k_new || !v_new) return fail(FLOWMM_EINVAL, "k_new and v_new must not be NULL");
   if (misaligned(k_new) || misaligned(v_new)) return fail(FLOWMM_EINVAL, "k_new and v_new must be 16-byte aligned");
-  if (p->n_kv_heads > 32767) return fail(FLOWMM_EUNSUPPORTED, "more than 32767 kv heads");
   AppendQuantCall c;
   c.k_codes = cache->k_codes; c.v_codes = cache->v_codes; c.k_scales = cache->k_scales; c.v_scales = cache->v_scales;
   c.k_new = k_new; c.v_new = v_new;
@@ -1095,7 +1109,7 @@ FLOWMM_API flowmm_status flowmm_cache_attention_quantized(const flowmm_params *p
   flowmm_status st = check_cache(p, cu_capacity, lengths);
   if (st != FLOWMM_OK) return st;
   if (!lengths) return fail(FLOWMM_EINVAL, "lengths must not be NULL");
-  if ((st = check_quantized(p, cache)) != FLOWMM_OK) return st;
+  if ((st = check_quantized(p, cache, false)) != FLOWMM_OK) return st;
   CacheAttnArgs a;
   a.K_c = cache->k_codes; a.V_c = cache->v_codes; a.k_scales = cache->k_scales; a.v_scales = cache->v_scales;
   a.ks_layer = cache->stride_layer / 16; a.ks_head = cache->stride_head / 16; a.ks_tok = cache->stride_token / 16;

@@ -51,6 +51,7 @@ COMMON = [
     (dict(), dict(lengths=[-1, 50]), "outside", fb.FLOWMM_EINVAL),
     (dict(), dict(cap=[0, 40, 30]), "increasing", fb.FLOWMM_EINVAL),
     (dict(), dict(cap=[1, 40, 90]), "cu_capacity[0]", fb.FLOWMM_EINVAL),
+    (dict(), dict(cap=[0, 40, 2 ** 31 - 65536]), "rows", fb.FLOWMM_EUNSUPPORTED),
 ]
 CALLS = {
     "quantize": lambda p, cap, ln, c: fb.flowmm_cache_quantize(p, cap, ln, [0, 40], good, far[0], c),
@@ -92,7 +93,7 @@ def test_rows():
         fb.flowmm_cache_quantize(p, CAP, [30, 49], [0], good, far[0], Cache())
 
 
-SCORING = [(dict(cap=-1.0), "cap"), (dict(cap=float("nan")), "cap"), (dict(cap=float("inf")), "cap"), (dict(cap=1e-45), "cap"), (dict(slopes=good + 2), "slopes")]
+SCORING = [(dict(cap=-1.0), "cap"), (dict(cap=float("nan")), "cap"), (dict(cap=float("inf")), "cap"), (dict(cap=1e-45), "cap"), (dict(cap=1e-39), "cap"), (dict(cap=2e36), "cap"), (dict(slopes=good + 2), "slopes")]
 
 
 def test_attention_over_a_cache():
@@ -155,3 +156,14 @@ def test_integer_arrays_of_any_form():
     for values in ([3, 4], (3, 4), np.array([3, 4]), np.array([3, 9, 4, 9], np.int32)[::2]):
         s = fb.Scoring(prefix=values, q_pos=values, row_pos=good)
         assert [s.c.prefix[i] for i in range(2)] == [3, 4] and [s.c.q_pos[i] for i in range(2)] == [3, 4]
+
+
+def test_rows_that_would_share_a_place():
+    p = params()
+    for name in ("quantize", "append"):
+        for kw in (dict(stride_layer=0), dict(stride_head=0)):
+            refused(lambda: CALLS[name](p, CAP, [30, 49], Cache(**kw)), "one place")
+    for strides in ((0, 90 * 128, 128), (2 * 90 * 128, 0, 128)):
+        refused(lambda: CALLS["dequantize"](params(k_strides=strides), CAP, [30, 49], Cache()), "one place")
+    for rows in ([0, 29], [7, 7], [48, 0]):
+        refused(lambda: fb.flowmm_cache_dequantize(p, CAP, [30, 49], rows, Cache(), good, far[0]), "one place")
