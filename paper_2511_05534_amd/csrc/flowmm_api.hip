@@ -971,9 +971,9 @@ flowmm_status quantize_call(const flowmm_params *p, const int32_t *cu_capacity, 
 
 // Waves that share the query rows of the prompt's attention and split the keys, `items` being the groups of 32 rows (all heads, layers): one workgroup of eight waves has a
 // compute unit to itself.  Causal prompts end with short rows that fill gaps, so that the split is worth it up to twice the compute units (bf16, 128 channels, us in
-// one / two / four: 704 items of 675 tokens 25.8 / 17.3 / 18.0, 1216 of 1200 38 / 25 / 34, 2016 of 2000 58 / 43 / 62, 3008 of 3000 90 / 91 / 115; fp32, whose rounds
-// cost what they compute, 1064 of 1200 345 / 188 / 148, 2632 of 3000 846 / 690 / 777).  Rows that nearly all see as much (a prefix or a picture of most of the prompt)
-// take as many rounds as there are: 704 items of 675 tokens, 576 of them a picture, 34.6 / 25.5 / 31.0.
+// one / two / four: 704 items of 675 tokens 26 / 17 / 18, 1216 of 1200 38 / 25 / 37, 2016 of 2000 59 / 46 / 72, 3008 of 3000 92 / 95 / 141; fp32, whose rounds
+// cost what they compute, 1024 of 1000 279 / 163 / 115, 1600 of 1600 450 / 247 / 278, 3008 of 3000 839 / 793 / 861).  Rows that nearly all see as much (a prefix or a picture
+// of most of the prompt) take as many rounds as there are: 704 items of 675 tokens, 576 of them a picture, 27 / 21 / 27, 1216 of 1200 42 / 53 / 57, 2016 of 2000 76 / 88 / 121.
 int prompt_key_split(const flowmm_params *p, const int32_t *prefix, int image_spans, const Shape &sh, long long items) {
   if (items > 512 && items < 2048 && (prefix || image_spans)) {
     long long sum = 0, n = 0, most = 0;

@@ -312,14 +312,23 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
         for (int i = u ? 0 : 2; i < 16; i += 2) x = fmaxf(fmaxf(x, s[u][i]), s[u][i + 1]);
       return x;
     };
-    // Weights are exp2(score - maximum), taken as exp2(fma(s, mul, add - maximum)) with whatever is left in s: the product, where whole blocks are neither capped nor
+    auto mask = [&]() {
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        const int last = limit - key0 - 32 * u * KS - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[u][i] = acc_row(i, 0) <= last ? s[u][i] : -INFINITY;
+      }
+    };
+    // Weights are exp2(score - maximum), taken as exp2(fma(s, mul, add - maximum)) with whatever is left in s: the product, where it is neither capped nor
     // biased; -1 / (1 + e^(2 u)), where they are capped only (the cap's own rounding is larger); the score.  A product's fused multiply-add keeps what the maximum's
     // rounding lost, 2^-24 of it: nothing where scores are within 2^24, an overflow at 1e30.  Larger ones (or NaN) are rounded first.
     float mul = 1.f, add = 0.f, tm = 0.f;
     bool ready = false;
-    if constexpr (!MASKED && !SCORED) {
+    if constexpr (!SCORED && (BF16 || !MASKED)) {
+      if constexpr (MASKED) mask();
       tm = most();
-      ready = !__any(!(fabsf(tm) * a.score.cl < 0x1p24f));
+      ready = !__any(!(fabsf(tm) * a.score.cl < 0x1p24f) && !(MASKED && tm == -INFINITY));
       if (ready) mul = a.score.cl;
     }
     if (!ready) {
@@ -335,14 +344,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
 #pragma unroll
         for (int u = 0; u < NB; ++u) score<SCORED, !BF16>(a, s[u], slope, key0 + 32 * u * KS + 4 * half, p0 + n);
       }
-      if constexpr (MASKED) {
-#pragma unroll
-        for (int u = 0; u < NB; ++u) {
-          const int last = limit - key0 - 32 * u * KS - 4 * half;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] = acc_row(i, 0) <= last ? s[u][i] : -INFINITY;
-        }
-      }
+      if constexpr (MASKED && (SCORED || !BF16)) mask();
       tm = most();
     }
     tm = fmaf(tm, mul, add);
@@ -386,21 +388,28 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
               __builtin_memcpy(reinterpret_cast<char *>(&vf[c]) + 8 * jj, &v, 8);
             }
           if constexpr (MASKED) {
+            typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_t;
+            u16x2_t most_v = {0, 0};  // magnitudes, as numbers of 15 bits
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-              unsigned *w = reinterpret_cast<unsigned *>(&vf[c]);
+            for (int c = 0; c < CT; ++c)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const bool hi = (w[e] & 0x7f800000u) == 0x7f800000u, lo = (w[e] & 0x7f80u) == 0x7f80u;
-                odd |= hi | lo;
-                w[e] = (hi ? 0u : w[e] & 0xffff0000u) | (lo ? 0u : w[e] & 0xffffu);
+                const unsigned w = reinterpret_cast<const unsigned *>(&vf[c])[e] & 0x7fff7fffu;
+                most_v = __builtin_elementwise_max(most_v, __builtin_bit_cast(u16x2_t, w));
+              }
+            if (__any(max(most_v.x, most_v.y) >= 0x7f80)) {
+              odd = true;
+#pragma unroll
+              for (int c = 0; c < CT; ++c) {
+                unsigned *w = reinterpret_cast<unsigned *>(&vf[c]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  w[e] = ((w[e] & 0x7f800000u) == 0x7f800000u ? 0u : w[e] & 0xffff0000u) | ((w[e] & 0x7f80u) == 0x7f80u ? 0u : w[e] & 0xffffu);
               }
             }
           }
-
 #pragma unroll
           for (int c = 0; c < CT; ++c) mma_chunk<true>(o[c], vf[c], pf);
-
         }
       } else {
 #pragma unroll
@@ -420,17 +429,18 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
     if constexpr (MASKED) {
       if (__any(odd)) {
 #pragma unroll 1
-        for (int j = 0; j < 32; ++j) {
-          if (key0 + j >= L) break;
+        for (int j = 0; j < 32 * NB; ++j) {
+          const int row = 32 * kb + (j & 31) + 32 * KS * (j >> 5), key = t * KT + row;
+          if (key >= L) break;
 #pragma unroll
           for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int ch = 32 * c + acc_row(i, half);
               float v;
-              if constexpr (BF16) v = bf16_bits_to_float(*lds_at<uint16_t>(values + VT::slot(32 * kb + j, ch >> 3) * 16 + 2 * (ch & 7)));
-              else v = *lds_at<float>(values + VT::slot(32 * kb + j, ch >> 2) * 16 + 4 * (ch & 3));
-              if (!(fabsf(v) < INFINITY) && key0 + j <= limit) o[c][i] += v;
+              if constexpr (BF16) v = bf16_bits_to_float(*lds_at<uint16_t>(values + VT::slot(row, ch >> 3) * 16 + 2 * (ch & 7)));
+              else v = *lds_at<float>(values + VT::slot(row, ch >> 2) * 16 + 4 * (ch & 3));
+              if (!(fabsf(v) < INFINITY) && key <= limit) o[c][i] += v;
             }
         }
       }
@@ -442,15 +452,19 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
     __builtin_amdgcn_s_waitcnt(0);  // this wave's part of tile t has landed
     __syncthreads();                // ... and everybody else's; tile t-1 is no longer read
     if (t + 1 < ntiles) request(t + 1);
-    // blocks of 32 keys: those that all of the wave's rows see whole, two at a time, then the others, one by one
-    const int full = min(max((w_first + 1 - t * KT) >> 5, 0), KT / 32);
+    // blocks of 32 keys: those that all of the wave's rows see whole, then the others; two at a time
+    const int full = min(max((w_first + 1 - t * KT) >> 5, 0), KT / 32), seen = min((w_last - t * KT + 32) >> 5, KT / 32);
     int kb = ks;
 #pragma unroll 1
     for (; BF16 && kb + KS < full; kb += 2 * KS) blocks(std::integral_constant<int, 2>{}, std::false_type{}, t, kb);
+    if constexpr (!BF16) {
 #pragma unroll 1
-    for (; kb < full; kb += KS) blocks(std::integral_constant<int, 1>{}, std::false_type{}, t, kb);
+      for (; kb < full; kb += KS) blocks(std::integral_constant<int, 1>{}, std::false_type{}, t, kb);
+    }
 #pragma unroll 1
-    for (; kb < KT / 32 && t * KT + 32 * kb <= w_last; kb += KS) blocks(std::integral_constant<int, 1>{}, std::true_type{}, t, kb);
+    for (; BF16 && kb + KS < seen; kb += 2 * KS) blocks(std::integral_constant<int, 2>{}, std::true_type{}, t, kb);
+#pragma unroll 1
+    for (; kb < seen; kb += KS) blocks(std::integral_constant<int, 1>{}, std::true_type{}, t, kb);
   }
 
   store_rows<BF16, D, KS>(a, w, o, m, z, reinterpret_cast<float *>(lds_kv));
