@@ -2,7 +2,9 @@
 // (bf16, fp32) or e4m3 codes with a scale per block of 32 (flowmm_cache_attention, flowmm_cache_attention_quantized).
 //
 // What bounds it is the stream of K and V rows: 2 * d bytes a row in 8 bits, two and four times that in bf16 and fp32; the products of
-// up to 16 query heads with a row take a tenth of the time in which it arrives.  Every wave works through tiles of 16 or 32 rows of its
+// up to 16 query heads with a row take a tenth of the time in which it arrives.  32 sequences of up to 16384 rows in 8 bits, 4 layers x 32/8 heads: 496 us,
+// 5.7 TB/s of the 5.9 that plain reads reach here; 3688 bf16 rows of 32 x 32/8 heads: 89 us, 5.5 TB/s.  Small calls are trips to memory one after the other:
+// 450 rows of 28 x 28/4, 13 MB, 8.1 us.  fp32 rows (4 sequences of up to 900, 8 layers x 16/4 heads, 64 channels: 16.5 us) also wait for their 32 products of 16x16x4 a tile.  Every wave works through tiles of 16 or 32 rows of its
 // own, with one K and one V buffer in LDS that it refills by direct global->LDS loads (whole rows, no registers) as soon as the matrix
 // operands have been read out of them, and no barrier until the end.
 //   logits  : S[key][head] = K tile x queries.  Which channels share a k slot of the instruction is free as long as both operands agree:

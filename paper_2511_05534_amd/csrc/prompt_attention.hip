@@ -7,7 +7,15 @@
 // rows in their lanes, so that a row's statistics are a lane's own and P is, register for register, an operand of O^T = V^T P^T.  The eight
 // waves of a workgroup take the heads of the kv group at the same rows first and walk over one stream of K and V tiles, which direct
 // global->LDS loads fill, double buffered.  V comes out of LDS transposed (ds_read_b64_tr_b16; fp32: by ordinary reads).
-// Where rows are few, two or four waves share them and split the keys.
+// Where rows are few, two or four waves share them and split the keys.  32 rows and 128 keys at a time: 64 rows a wave would leave no registers for two waves on a SIMD,
+// and one wave's matrix instructions do not cover its own softmax.
+//
+// What bounds it: matrix cores (512 cycles of 32 keys x 32 rows at 128 channels) and vector issue (about 400: per logit an exponential at a quarter of the rate, a multiply-add,
+// half a maximum, half an addition, half a conversion) of the two waves of a SIMD, which overlap in part, and the power limit (2.0 GHz).  16384 tokens, 32/8 heads, bf16:
+// 2030 us, 1.08 PFLOP/s of the 1.21 that a large product of the library reaches; matrix cores busy 52 % of the time.  8 sequences of up to 8192, capped, 28/4 heads: 1780 us,
+// 0.82 PFLOP/s (two exponentials and a reciprocal per logit).  675 tokens, 32 heads: 17 us, 20 with a picture in them; the workgroup of a block of rows that only in part see
+// the picture is the last one.  The loads cost nothing that shows (all from one tile: 3 % less).  Blocks that some rows see in part take the same path with a mask, two at
+// a time as well (one by one, each of V's numbers filtered: 675 tokens with a picture 25.4 us).
 //
 // bf16: P is rounded to bf16 for the second product, as V is one (relative 2^-9 a weight, each its own, so that it stays below the
 // rounding of the result wherever many keys count); its sum is of the fp32 weights.  fp32: both products by the fp32 matrix instructions.
@@ -24,7 +32,10 @@ namespace flowmm {
 namespace {
 
 constexpr int kPThreads = kPromptWaves * 64;
-constexpr int kPromptGroupWgs = 4096;  // workgroups of a group of units
+// Workgroups of a group of units: as many as compute units, so that the workgroups of a unit run together and its keys and values are fetched once (a unit stays on an XCD).
+// Groups of 8 units / 128 workgroups / 256 / 512 / 1024 / 4096, us: 256 units x 2048 tokens 407 / 362 / 350 / 348 / 367 / 387, 512 x 1100 300 / 296 / 308 / 316 / 331 / 338, 1024 x 400
+// 184 / 157 / 163 / 172 / 173 / 173, 112 x 675 (28/4 heads) 182 / 182 / 181 / 183 / 190 / 195; 8 units of 16384 tokens the same throughout.
+constexpr int kPromptGroupWgs = 256;
 
 // V rows in LDS: whole rows by direct loads as in KeyTile, the chunks of a row permuted so that the four rows that 16 lanes transpose, 32 bytes
 // of each, lie in different banks
