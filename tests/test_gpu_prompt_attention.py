@@ -232,6 +232,30 @@ def test_what_a_token_does_not_see_does_not_reach_it(dtype, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("L, hq", [(400, 1), (700, 40), (900, 140)])  # keys split over four waves, two, one
+def test_infinities_in_pictures_of_many_blocks(dtype, cap, L, hq):
+    """The first block of rows sees the picture in part: its text rows get what they get without the picture's infinities, bit for bit."""
+    a = Prompt(dtype, 1, hq, hq, 64, [L], cap=cap, spans=[[(0, 20, 0), (20, L - 30, 1), (L - 30, L, 0)]], image_spans=True, seed=24)
+    a.run()
+    torch.cuda.synchronize()
+    clean = a.out.cpu().float()
+    places = [(25, 3, float("inf"), 20), (L // 2, 5, float("-inf"), 20), (L // 2 + 33, 5, float("-inf"), 20), (L - 40, 7, float("nan"), 20), (L - 10, 9, float("inf"), L - 10)]
+    for row, ch, x, _ in places:
+        a.V[0, :, row, ch] = x
+    a.upload()
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu().float()
+    for _, ch, x, first in places:
+        o = got[0, :, first:, ch]
+        assert (o.isnan() if x != x else o == x).all(), (ch, x)
+    for _, ch, _, first in places:
+        got[0, :, first:, ch] = clean[0, :, first:, ch]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_lowest_values_in_the_logits(dtype):
     """Logits of the lowest finite size and of -infinity beside ordinary ones: they weigh nothing."""
     a = Prompt(dtype, 1, 1, 1, 64, [40], seed=12)
