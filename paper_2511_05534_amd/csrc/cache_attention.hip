@@ -266,8 +266,8 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
         float rest = p[u][i];
 #pragma unroll
         for (int k = 0; k < kTerms; ++k) {
-          // (bf16 rows may be infinite: a term of 0 would make NaN of them; 2^-126 is far below the rounding of any sum with a weight of 1 in it)
-          if (R == kRowBF16 && k > 0) rest = fmaxf(rest, FLT_MIN);
+          // (bf16 rows may be infinite: a term of 0 would make NaN of them where the weight is not 0)
+          if (R == kRowBF16 && k > 0) rest = at_least_a_term(rest, term[u][0][i]);
           term[u][k][i] = __float_as_uint(rest) & (k + 1 < kTerms ? 0xffff0000u : 0xffffffffu);
           if (k + 1 < kTerms) rest -= __uint_as_float(term[u][k][i]);
         }

@@ -41,6 +41,12 @@ __device__ __forceinline__ float quad_sum(float v) {
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+// A later bf16 term of a weight whose first one is `first` (bits): the smallest subnormal bf16, 2^-133, at the least, which the matrix cores
+// keep and which times infinity is infinity; 0 where the weight is 0, whose product with the largest V has to be 0.
+__device__ __forceinline__ float at_least_a_term(float rest, unsigned first) {
+  return __uint_as_float(max(__float_as_uint(rest), min(first, 0x10000u)));
+}
+
 // ---- tasks: `chunk` slots of one (sequence, kv head, layer) for a workgroup ----
 constexpr int kDecodeTail = 1024;  // four per compute unit (512: 0 to 3 us slower, 2048 to all: 0 to 9)
 

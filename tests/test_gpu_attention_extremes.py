@@ -1,0 +1,41 @@
+"""The scored attentions at the ends of the ranges of their inputs, and key by key, against plain 64-bit forms."""
+import pytest
+import torch
+
+import attention_reference as ref
+from paper_2511_05534_amd import binding as fb
+from test_gpu_prompt_attention import Prompt
+from test_gpu_quantized_cache import DEV, DT, KINDS, Attention, params, stream
+
+pytestmark = pytest.mark.gpu
+
+
+def upload(a):
+    """The rows and queries that a test has changed on the CPU, to the GPU."""
+    a.qd.copy_(a.q.to(DEV))
+    if a.rows != "fp8":
+        a.dev[0].copy_(a.K.to(DEV))
+        a.dev[1].copy_(a.V.to(DEV))
+        return
+    Kd, Vd = a.K.to(DEV), a.V.to(DEV)
+    src = params(a.layers, a.hq, a.hkv, a.d, a.dtype, a.caps)
+    fb.flowmm_cache_quantize(src, a.cu, a.caps, a.cu, Kd.data_ptr(), Vd.data_ptr(), a.cache, stream())
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("rows, dtype", KINDS)
+@pytest.mark.parametrize("lens", [[90], [700, 130], [9000]])
+@pytest.mark.parametrize("below", [1000.0, 60.0])
+def test_large_values_that_weigh_little(rows, dtype, lens, below):
+    """V near the type's largest number in rows whose logit is so far below the others' that their weight is 0, or exp(-60)."""
+    a = Attention(rows, dtype, 1, 4, 2, 64, lens, scale=0.125, seed=15)
+    a.q[:] = 0.0
+    a.q[..., 0] = 8.0
+    a.K[:] = 0.0
+    for b, n in enumerate(lens):
+        far = torch.arange(a.cu[b] + 5, a.cu[b] + n, 64)  # (one in a tile: the sum of a tile of them would leave fp32's range)
+        a.K[:, :, far, 0] = -below
+        a.V[:, :, far] = (3e38 * torch.tensor([1.0, -1.0, 0.5, 1.0]).repeat(len(far))[:len(far), None]).to(a.V.dtype)
+    upload(a)
+    a.run()
+    a.check(f"{rows} {dtype} {lens} below {below}")
