@@ -1211,3 +1211,34 @@ def test_sequences_by_length(oracle, lens, heads, layers, d):
         gpu = run_gpu(w, fused=fused, flags=1)
         for l in (0, layers // 2, layers - 1):
             check_layer(oracle, w, gpu, l, flags=1)
+
+
+@pytest.mark.parametrize("dtype,d,B", [("bf16", 64, 40), ("bf16", 128, 200), ("bf16", 128, 900), ("f32", 64, 40), ("f32", 128, 200)])
+@pytest.mark.parametrize("below", [1000.0, 60.0])
+def test_decode_attention_of_large_values_that_weigh_little(dtype, d, B, below):
+    """V near the type's largest number in rows whose logit is so far below the others' that their weight is 0, or exp(-60)."""
+    import torch
+    fb = _fb()
+    print(f"{dtype} d {d} B {B} below {below}", flush=True)
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    params = fb.Params(1, 2, 1, d, dtype, [B], [B], [[(0, B, 0)]], 1, 0.25, [1.0], scale=0.125)
+    bufs = fb.DeviceBuffers(params)
+    gen = torch.Generator(device="cuda:0").manual_seed(6)
+    bufs.V_out.normal_(generator=gen)
+    bufs.K_out.zero_()
+    V = bufs.V_out[0, 0]
+    far = [1, 7, 18, B - 1]
+    bufs.K_out[0, 0, far, 0] = -below
+    V[far] = torch.tensor([1.0, -1.0, 1.0, -0.5], device="cuda:0", dtype=tdt)[:, None] * 3e38
+    q = torch.zeros((1, 2, 1, d), dtype=tdt, device="cuda:0")
+    q[..., 0] = 8.0
+    out = torch.empty_like(q)
+    bufs.decode_attention(q, out, stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    Vd, got = V.double().cpu().numpy(), out[0, :, 0].double().cpu().numpy()
+    p = np.ones(B)
+    p[far] = np.exp(-below)
+    want, size = p @ Vd / p.sum(), p @ np.abs(Vd) / p.sum()
+    # the result's rounding; a weight's: of its logit (exactly 0 or -below, times log2 e, 2^-24 twice) and of exp2, 2^-22, and the sums' B 2^-24
+    tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) * 1.01 + (2 * below * 2.0 ** -24 + 2.0 ** -21 + 2 * B * 2.0 ** -24) * size
+    assert (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
