@@ -262,7 +262,8 @@ typedef struct {
  * other.  K, V through p's k strides; Q_full and out [Lyr][Hq][T][d] through the three strides given
  * (elements; head_dim contiguous; 32 consecutive tokens of a head must lie within 4 GiB,
  * FLOWMM_EUNSUPPORTED otherwise); out must not overlap the inputs.  What a token does not see does not
- * reach it, infinities and NaN included.  The weights of bf16 calls are rounded to bf16 for the product with V (their
+ * reach it, infinities and NaN included; what it sees counts by its weight, so that an infinity whose
+ * weight is 0 leaves a NaN.  The weights of bf16 calls are rounded to bf16 for the product with V (their
  * sum is not), all sums are fp32.  p, workspace (size from flowmm_plan_sizes), stream and errors as for
  * flowmm_plan; window, budgets, tau and theta are validated but not used. */
 flowmm_status flowmm_prompt_attention(const flowmm_params *p, const flowmm_scoring *scoring, const void *K, const void *V,

@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
       }
       z += za + zb;
     }
-    // ---- O += V^T P; a masked block's infinite or undefined values may only reach the rows that see them: taken out here, added below ----
+    // ---- O += V^T P; a masked block's infinite or undefined values may only reach the rows that see them: taken out here, added with their weights below ----
     bool odd = false;
 #pragma unroll
     for (int u = 0; u < NB; ++u) {
@@ -439,10 +439,17 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
     }
     if constexpr (MASKED) {
       if (__any(odd)) {
+        // (as in a whole block: infinite, and undefined where the weight is 0)
 #pragma unroll 1
         for (int j = 0; j < 32 * NB; ++j) {
           const int row = 32 * kb + (j & 31) + 32 * KS * (j >> 5), key = t * KT + row;
           if (key >= L) break;
+          float weight = 0.f;  // of key j, in the lanes of the half-wave that holds it
+#pragma unroll
+          for (int u = 0; u < NB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) weight = 32 * u + acc_row(i, 0) == (j & ~4) ? s[u][i] : weight;
+          weight = __shfl(weight, n + 8 * (j & 4), 64);
 #pragma unroll
           for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -451,7 +458,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prompt_attention_kernel(KernelAr
               float v;
               if constexpr (BF16) v = bf16_bits_to_float(*lds_at<uint16_t>(values + VT::slot(row, ch >> 3) * 16 + 2 * (ch & 7)));
               else v = *lds_at<float>(values + VT::slot(row, ch >> 2) * 16 + 4 * (ch & 3));
-              if (!(fabsf(v) < INFINITY) && key <= limit) o[c][i] += v;
+              if (!(fabsf(v) < INFINITY) && key <= limit) o[c][i] += weight * v;
             }
         }
       }

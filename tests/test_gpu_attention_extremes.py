@@ -39,3 +39,31 @@ def test_large_values_that_weigh_little(rows, dtype, lens, below):
     upload(a)
     a.run()
     a.check(f"{rows} {dtype} {lens} below {below}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [0.0, 2000.0])
+@pytest.mark.parametrize("L, hq", [(400, 1), (700, 40), (900, 140)])  # keys split over four waves, two, one
+@pytest.mark.parametrize("below", [1000.0, 20.0])
+def test_prompt_infinite_values_that_weigh_little(dtype, cap, L, hq, below):
+    """An infinite value times its weight: infinite where the weight is small, undefined where it is 0, whichever way the row's blocks are taken."""
+    a = Prompt(dtype, 1, hq, hq, 64, [L], cap=cap, scale=0.125, spans=[[(0, 20, 0), (20, L - 150, 1), (L - 150, L, 0)]], image_spans=True, seed=25)
+    a.Q[:] = 0.0
+    a.Q[..., 0] = 8.0
+    a.K[:] = 0.0
+    # key, channel, value, first row that sees it
+    places = [(10, 1, float("inf"), 10), (25, 3, float("inf"), 20), (L // 2, 5, float("-inf"), 20), (L - 160, 7, float("nan"), 20), (L - 120, 9, float("inf"), L - 120),
+              (L - 65, 11, float("-inf"), L - 65), (L - 2, 13, float("inf"), L - 2)]
+    for row, ch, x, _ in places:
+        a.V[0, :, row, ch] = x
+        a.K[0, :, row, 0] = -below
+    a.upload()
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu().float()
+    other = [c for c in range(64) if c not in [p[1] for p in places]]
+    assert torch.isfinite(got[..., other]).all()
+    for _, ch, x, first in places:
+        o = got[0, :, :, ch]
+        assert torch.isfinite(o[:, :first]).all(), ch
+        assert (o[:, first:].isnan() if below > 100 or x != x else o[:, first:] == x).all(), (ch, x)
