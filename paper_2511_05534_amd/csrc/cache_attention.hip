@@ -134,7 +134,10 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
   int r0 = s0 + wave * TR;
   const int *pos = POS ? a.row_pos + unit * a.SB + s.slot : nullptr;
   auto request_k = [&](int r) {
-    if constexpr (POS) load_to_lds<4>(pos, (unsigned)min(r + (lane & (TR - 1)), s.merged - 1) * 4u, tp);
+    if constexpr (POS) {
+      const int first = min(r, s.merged - 1);  // (offsets of 32 bits from the tile's first position)
+      load_to_lds<4>(pos + first, (unsigned)min(lane & (TR - 1), s.merged - 1 - first) * 4u, tp);
+    }
     request_rows<R, D>(Kc + (long long)r * a.ks_tok, a.ks_tok, s1 - r, tk);
   };
   auto request_v = [&](int r) { request_rows<R, D>(Vc + (long long)r * a.ks_tok, a.ks_tok, s1 - r, tv); };

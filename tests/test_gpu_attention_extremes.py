@@ -67,3 +67,32 @@ def test_prompt_infinite_values_that_weigh_little(dtype, cap, L, hq, below):
         o = got[0, :, :, ch]
         assert torch.isfinite(o[:, :first]).all(), ch
         assert (o[:, first:].isnan() if below > 100 or x != x else o[:, first:] == x).all(), (ch, x)
+
+
+@pytest.fixture
+def much_memory():
+    """Memory that later tests do not find taken."""
+    yield lambda gib: torch.cuda.mem_get_info()[0] >= gib << 30 or pytest.skip("not enough memory")
+    torch.cuda.empty_cache()
+
+
+def test_positions_of_more_than_two_to_the_thirty_rows(much_memory):
+    """The bias of merged rows whose positions lie more than 4 GiB behind the first one's: the last rows alone are near the query."""
+    d, n, near, q_pos = 64, (1 << 30) + 1000, 700, 1 << 29
+    much_memory(80)
+    p = params(1, 1, 1, d, "bf16", [n], [n])
+    cu = [0, n]
+    codes = torch.zeros((1, 1, n, d), dtype=torch.uint8, device=DEV)
+    codes[0, 0, n - near:] = 0x38  # 1, in the rows near the query
+    codes = codes.view(torch.float8_e4m3fn)
+    scales = torch.ones((1, 1, -(-n // 32)), device=DEV)
+    cache = fb.QuantizedCache(p, cu, tensors=[codes, codes, scales, scales])
+    pos = torch.zeros(n, dtype=torch.int32, device=DEV)
+    pos[n - near:] = q_pos
+    slopes = torch.ones(1, device=DEV)
+    q, out = torch.zeros((1, 1, 1, d), dtype=torch.bfloat16, device=DEV), torch.full((1, 1, 1, d), 9.0, dtype=torch.bfloat16, device=DEV)
+    size = fb.flowmm_cache_sizes(p, cu)[2]
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    scoring = fb.Scoring(slopes=slopes.data_ptr(), row_pos=pos.data_ptr(), q_pos=[q_pos])
+    fb.flowmm_cache_attention_quantized(p, cu, [n], scoring, q.data_ptr(), cache, out.data_ptr(), ws.data_ptr(), size, stream())
+    assert (out == 1.0).all(), out
