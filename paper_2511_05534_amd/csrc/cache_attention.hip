@@ -503,7 +503,7 @@ hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnCall &c, hipSt
       const int b = a.b0 + i;
       const int merged = a.row_pos ? c.budgets[b] : 0;
       a.cu[i] = CacheAttnArgs::Seq{a.tasks, len[i], c.cu_capacity[b], block, merged, slot, a.row_pos ? c.q_pos[b] : 0, 0};
-      a.tasks += len[i] <= a.chunk ? 1 : (len[i] + a.chunk - 1) / a.chunk;
+      a.tasks += len[i] <= a.chunk ? 1 : (len[i] - 1) / a.chunk + 1;  // (a length and a part's may add up to more than an int holds)
       block += (c.cu_capacity[b + 1] - c.cu_capacity[b] + kQuantRows - 1) / kQuantRows;
       slot += merged;
       sum += len[i];

@@ -96,3 +96,22 @@ def test_positions_of_more_than_two_to_the_thirty_rows(much_memory):
     scoring = fb.Scoring(slopes=slopes.data_ptr(), row_pos=pos.data_ptr(), q_pos=[q_pos])
     fb.flowmm_cache_attention_quantized(p, cu, [n], scoring, q.data_ptr(), cache, out.data_ptr(), ws.data_ptr(), size, stream())
     assert (out == 1.0).all(), out
+
+
+def test_a_sequence_of_nearly_two_to_the_thirty_one_rows(much_memory):
+    """The longest sequence there is, in the most parts: its length and a part's do not add up to an int."""
+    d, n, near = 64, (1 << 31) - 65537, 40
+    much_memory(150)
+    p = params(1, 1, 1, d, "bf16", [n])
+    cu = [0, n]
+    codes = torch.zeros((1, 1, n, d), dtype=torch.uint8, device=DEV)
+    codes[0, 0, n - near:] = 0x38  # 1, in the rows near the query
+    codes = codes.view(torch.float8_e4m3fn)
+    scales = torch.ones((1, 1, -(-n // 32)), device=DEV)
+    cache = fb.QuantizedCache(p, cu, tensors=[codes, codes, scales, scales])
+    slopes = torch.full((1,), 4.0, device=DEV)
+    q, out = torch.zeros((1, 1, 1, d), dtype=torch.bfloat16, device=DEV), torch.full((1, 1, 1, d), 9.0, dtype=torch.bfloat16, device=DEV)
+    size = fb.flowmm_cache_sizes(p, cu)[2]
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    fb.flowmm_cache_attention_quantized(p, cu, [n], fb.Scoring(slopes=slopes.data_ptr()), q.data_ptr(), cache, out.data_ptr(), ws.data_ptr(), size, stream())
+    assert (out == 1.0).all(), out  # the rows behind them weigh exp(-160) and less
