@@ -128,7 +128,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
   f32x4_t acc[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  // of head n; z over this lane's keys only.  The maximum starts finite: rows whose logits are all -inf weigh 0, not NaN
+  // of head n; z over this lane's keys only.  The maximum starts finite: rows whose logit is -inf weigh 0, not NaN, also where a wave sees no others (a query that sees no others gets 0 / 0)
   float m = -FLT_MAX, z = 0.f;
   const int step = WAVES * TR;
   int r0 = s0 + wave * TR;

@@ -115,3 +115,46 @@ def test_a_sequence_of_nearly_two_to_the_thirty_one_rows(much_memory):
     ws = torch.empty(size, dtype=torch.uint8, device=DEV)
     fb.flowmm_cache_attention_quantized(p, cu, [n], fb.Scoring(slopes=slopes.data_ptr()), q.data_ptr(), cache, out.data_ptr(), ws.data_ptr(), size, stream())
     assert (out == 1.0).all(), out  # the rows behind them weigh exp(-160) and less
+
+
+def check_where_seen(a, got, q, K, V, hidden, dtype, weight_error, what):
+    """One head's rows against the 64-bit form over the keys that are not hidden (whose logits are -infinity)."""
+    want, tol = ref.attend(q, K.nan_to_num(0.0, 0.0, 0.0), V, a.scale, 0.0, None, None, hidden, DT[dtype], weight_error)
+    ref.check(got, want, tol, what)
+
+
+@pytest.mark.parametrize("rows, dtype", [k for k in KINDS if k[0] != "fp8"])
+@pytest.mark.parametrize("lens", [[40, 50], [9000, 600]])  # whole, cut into parts
+def test_logits_that_are_all_minus_infinity(rows, dtype, lens):
+    """0 / 0 where every logit is -infinity; where some are not, the others weigh nothing, also where they are all that a workgroup sees."""
+    a = Attention(rows, dtype, 1, 4, 2, 64, lens, seed=16)
+    a.q[..., 0] = 1.0
+    a.K[0, 0, :a.cu[1], 0] = float("-inf")                       # sequence 0, kv head 0: all
+    a.K[0, 1, :lens[0] * 3 // 5, 0] = float("-inf")              # kv head 1: the first three fifths
+    a.K[0, :, a.cu[1] + 5:a.cu[1] + lens[1], 0] = float("-inf")  # sequence 1: all but five
+    upload(a)
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu()
+    for b, n in enumerate(lens):
+        r = slice(a.cu[b], a.cu[b] + n)
+        for h in range(4):
+            K = a.K[0, h // 2, r]
+            check_where_seen(a, got[0, h, b][None], a.q[0, h, b][None], K, a.V[0, h // 2, r], K[:, 0].isinf()[None], dtype, 2.0 ** -15 if dtype == "bf16" else 0.0, (b, h))
+    assert got[0, :2, 0].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L, hq", [(400, 1), (700, 40), (900, 140)])  # keys split over four waves, two, one
+def test_prompt_logits_that_are_all_minus_infinity(dtype, L, hq):
+    a = Prompt(dtype, 1, hq, hq, 64, [L], seed=26)
+    a.Q[..., 0] = 1.0
+    a.K[0, :, :L // 2 + 3, 0] = float("-inf")
+    a.upload()
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu()
+    for h in (0, hq - 1):
+        hidden = a.hidden(0) | a.K[0, h, :, 0].isinf()[None]
+        check_where_seen(a, got[0, h], a.Q[0, h], a.K[0, h], a.V[0, h], hidden, dtype, 2.0 ** -8 if dtype == "bf16" else 0.0, h)
+    assert got[0, :, :L // 2 + 3].isnan().all()

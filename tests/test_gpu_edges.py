@@ -1242,3 +1242,21 @@ def test_decode_attention_of_large_values_that_weigh_little(dtype, d, B, below):
     # the result's rounding; a weight's: of its logit (exactly 0 or -below, times log2 e, 2^-24 twice) and of exp2, 2^-22, and the sums' B 2^-24
     tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) * 1.01 + (2 * below * 2.0 ** -24 + 2.0 ** -21 + 2 * B * 2.0 ** -24) * size
     assert (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
+
+
+@pytest.mark.parametrize("dtype,B", [("bf16", 40), ("bf16", 900), ("f32", 40), ("f32", 900)])
+def test_decode_attention_of_logits_that_are_all_minus_infinity(dtype, B):
+    """0 / 0, not an infinity."""
+    import torch
+    fb = _fb()
+    params = fb.Params(1, 2, 2, 64, dtype, [B], [B], [[(0, B, 0)]], 1, 0.25, [1.0])
+    bufs = fb.DeviceBuffers(params)
+    gen = torch.Generator(device="cuda:0").manual_seed(7)
+    bufs.K_out.normal_(generator=gen)
+    bufs.V_out.normal_(generator=gen)
+    bufs.K_out[0, 0, :, 0] = float("-inf")
+    q = torch.ones((1, 2, 1, 64), dtype=bufs.K_out.dtype, device="cuda:0")
+    out = torch.empty_like(q)
+    bufs.decode_attention(q, out, stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert out[0, 0].isnan().all() and torch.isfinite(out[0, 1]).all()
