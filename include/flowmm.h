@@ -267,7 +267,9 @@ typedef struct {
  * reach it, infinities and NaN included; what it sees counts by its weight, so that an infinity whose
  * weight is 0 leaves a NaN.  The weights of bf16 calls are rounded to bf16 for the product with V (their
  * sum is not), all sums are fp32.  p, workspace (size from flowmm_plan_sizes), stream and errors as for
- * flowmm_plan; window, budgets, tau and theta are validated but not used. */
+ * flowmm_plan; window (>= 1), budgets, tau and theta are not used.  Any number of query heads up to 1024, and prompts
+ * shorter than the window, are taken: where flowmm_plan_sizes refuses p for such a reason, the size that it reports
+ * for the same sequences and spans with window 1, n_q_heads = n_kv_heads and budgets of 1 is enough. */
 flowmm_status flowmm_prompt_attention(const flowmm_params *p, const flowmm_scoring *scoring, const void *K, const void *V,
                                       const void *Q_full, int64_t qf_stride_layer, int64_t qf_stride_head,
                                       int64_t qf_stride_token, void *out, void *workspace, size_t workspace_bytes,

@@ -996,6 +996,28 @@ int prompt_key_split(const flowmm_params *p, const int32_t *prefix, int image_sp
   return items >= 8 * 256 ? 1 : items >= 4 * 256 ? 2 : 4;
 }
 
+// Checks and sizes of a prompt's attention.  What flowmm_plan refuses for the sake of its windows and budgets (a prompt shorter than the window, too many of
+// the window's query rows or too many slots for LDS) is nothing to this call: it then needs the room for the description of the batch alone.
+flowmm_status prompt_layout(const flowmm_params *p, Layout &lo, size_t workspace_bytes) {
+  char message[sizeof(g_err)];
+  std::memcpy(message, g_err, sizeof(g_err));
+  const flowmm_status refused = build_layout(p, lo, workspace_bytes);
+  if (refused == FLOWMM_OK || !p || p->batch < 1 || !p->budget_tokens || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) return refused;
+  if (p->n_q_heads > 1024) return fail(FLOWMM_EUNSUPPORTED, "more than 1024 query heads");
+  const std::vector<int32_t> ones((size_t)p->batch, 1);
+  flowmm_params plain = *p;
+  plain.window = std::min(p->window, 1);
+  plain.n_q_heads = p->n_kv_heads;
+  plain.budget_tokens = ones.data();
+  const flowmm_status st = build_layout(&plain, lo);
+  if (st != FLOWMM_OK) return st;
+  std::memcpy(g_err, message, sizeof(g_err));  // (that of the last call that failed)
+  lo.sh.Hq = p->n_q_heads;
+  lo.sh.G = p->n_q_heads / p->n_kv_heads;
+  lo.workspace_bytes = lo.rg.mod;  // (behind the metadata)
+  return FLOWMM_OK;
+}
+
 // what the two cache attentions have in common; a.K_c .. and the strides are set
 flowmm_status cache_attention_call(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths, const flowmm_scoring *scoring, const void *q,
                                    void *out, void *workspace, size_t workspace_bytes, CacheAttnArgs &a, RowKind rows, void *stream) {
@@ -1120,7 +1142,7 @@ FLOWMM_API flowmm_status flowmm_prompt_attention(const flowmm_params *p, const f
                                       const void *Q_full, int64_t qf_stride_layer, int64_t qf_stride_head, int64_t qf_stride_token,
                                       void *out, void *workspace, size_t workspace_bytes, void *stream) {
   Layout lo;
-  flowmm_status st = build_layout(p, lo, workspace_bytes);
+  flowmm_status st = prompt_layout(p, lo, workspace_bytes);
   if (st != FLOWMM_OK) return st;
   const Shape &sh = lo.sh;
   if (!K || !V || !Q_full || !out || !workspace) return fail(FLOWMM_EINVAL, "K, V, Q_full, out and workspace must not be NULL");

@@ -167,3 +167,34 @@ def test_rows_that_would_share_a_place():
         refused(lambda: CALLS["dequantize"](params(k_strides=strides), CAP, [30, 49], Cache()), "one place")
     for rows in ([0, 29], [7, 7], [48, 0]):
         refused(lambda: fb.flowmm_cache_dequantize(p, CAP, [30, 49], rows, Cache(), good, far[0]), "one place")
+
+
+def test_prompt_attention_takes_layouts_that_the_plan_refuses():
+    """Its own limits are those of the queries' strides alone: what follows gets as far as the size of its workspace, which is that of the description of the batch."""
+    for kw in (dict(n_q_heads=48), dict(n_q_heads=1024, n_kv_heads=1), dict(window=41), dict(budgets=[0, 40]), dict(budgets=[41, 40]), dict(n_q_heads=48, head_dim=64, dtype="f32"),
+               dict(seqlens=[60000, 50], budgets=[60000, 40], spans=[[(0, 60000, 0)], [(0, 10, 0), (10, 50, 1)]])):
+        p = params(**kw)
+        with pytest.raises(fb.FlowMMError):
+            fb.flowmm_plan_sizes(p)
+        like = dict(kw, window=1, budgets=[1, 1], n_q_heads=kw.get("n_kv_heads", 2))
+        need = fb.flowmm_plan_sizes(params(**like))[1]
+        T, d = sum(kw.get("seqlens", [40, 50])), kw.get("head_dim", 128)
+        hq = kw.get("n_q_heads", 4)
+        places = [1 << 40, 1 << 44, 1 << 48, 1 << 52, 1 << 56]
+
+        def call(n, p=p, qs=(hq * T * d, T * d, d)):
+            return lambda: fb.flowmm_prompt_attention(p, None, places[0], places[1], places[2], qs, places[3], places[4], n)
+
+        refused(call(0), "workspace", fb.FLOWMM_EWORKSPACE)
+        with pytest.raises(fb.FlowMMError) as e:
+            call(255)()
+        assert int(e.value.message.split()[-2]) <= need, e.value.message
+        refused(call(need, qs=(hq * T * d, T * d, 8)), "head_dim")
+    for kw, word in ((dict(n_q_heads=2048, n_kv_heads=1), "1024"), (dict(n_q_heads=5), "multiple"), (dict(window=0), "window"), (dict(window=-3, budgets=[0, 0]), "window"), (dict(head_dim=96), "head_dim")):
+        with pytest.raises(fb.FlowMMError, match=word):
+            fb.flowmm_prompt_attention(params(**kw), None, good, far[0], far[1], (4 * 90 * 128, 90 * 128, 128), far[2], far[3], BIG)
+
+
+def test_the_last_error_is_that_of_a_call_that_failed():
+    refused(lambda: fb.flowmm_prompt_attention(params(window=0), None, good, far[0], far[1], (4 * 90 * 128, 90 * 128, 128), far[2], far[3], BIG), "window")
+    refused(lambda: fb.flowmm_prompt_attention(params(n_q_heads=48), None, good, far[0], far[1], (48 * 90 * 128, 90 * 128, 8), far[2], far[3], BIG), "head_dim")

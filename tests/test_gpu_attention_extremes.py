@@ -158,3 +158,21 @@ def test_prompt_logits_that_are_all_minus_infinity(dtype, L, hq):
         hidden = a.hidden(0) | a.K[0, h, :, 0].isinf()[None]
         check_where_seen(a, got[0, h], a.Q[0, h], a.K[0, h], a.V[0, h], hidden, dtype, 2.0 ** -8 if dtype == "bf16" else 0.0, h)
     assert got[0, :, :L // 2 + 3].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d, hq, hkv, lens, window", [(128, 40, 1, [70], 1), (128, 34, 2, [33, 5], 1), (64, 64, 1, [129], 1), (128, 6, 2, [3, 20, 100], 64), (64, 4, 4, [40], 5000)])
+def test_prompt_layouts_of_its_own(dtype, d, hq, hkv, lens, window):
+    """More query heads to a kv head than the plan takes, and prompts shorter than its window."""
+    a = Prompt(dtype, 2, hq, hkv, d, lens, cap=20.0, seed=27) if hq // hkv < 10 else None
+    if a is None:  # (the workspace of such a layout is that of one query head to a kv head)
+        one = Prompt(dtype, 2, hkv, hkv, d, lens, seed=27)
+        a = Prompt.__new__(Prompt)
+        a.__dict__.update(one.__dict__, hq=hq, scoring=None, cap=0.0)
+        a.Q = torch.randn((2, hq, sum(lens), d), generator=torch.Generator().manual_seed(28)).to(DT[dtype])
+        a.q_strides = (hq * sum(lens) * d, sum(lens) * d, d)
+        a.upload()
+    T = sum(lens)
+    a.p = fb.Params(2, hq, hkv, d, dtype, lens, lens, a.spans, window, 0.25, [1.0] * len(lens), k_strides=(hkv * T * d, T * d, d))
+    a.run()
+    a.check(f"{dtype} {d} {hq}/{hkv} {lens} window {window}")
