@@ -9,11 +9,11 @@
 // operands have been read out of them, and no barrier until the end.
 //   logits  : S[key][head] = K tile x queries.  Which channels share a k slot of the instruction is free as long as both operands agree:
 //             lane (n, q4) takes the 16-byte chunks 4 j + q4 of row n, so that every LDS read is 16 bytes
-//               codes: 16 of them, two v_mfma 16x16x32 after v_cvt_scalef32_pk_bf16_fp8 (exact); fp32 queries as three bf16 terms
+//               codes: 16 of them, two v_mfma 16x16x32 after v_cvt_scalef32_pk_bf16_fp8 with the block's scale (exact); fp32 queries as three bf16 terms
 //               bf16 : 8 channels, one 16x16x32;  fp32: 4 channels, four 16x16x4
-//   scores  : scale (times the block's K scale), cap, bias by distance in fp32, log2 domain
+//   scores  : scale, cap, bias by distance in fp32, log2 domain
 //   output  : O[channel][head] += V^T x p, p at the accuracy of the result: the two leading bf16 terms (2^-16) for bf16 results, three
-//             for fp32 ones, fp32 itself beside fp32 rows.  A block's V scale goes into p.  V comes out of LDS transposed
+//             for fp32 ones, fp32 itself beside fp32 rows.  V comes out of LDS transposed
 //             (ds_read_b64_tr_b8, _tr_b16), in the order of keys in which the accumulators of S hold p.
 // Rows past a sequence's end are read as its last one; their p is 0 and so are their V, whatever that row holds.
 #include <cfloat>
@@ -44,10 +44,19 @@ struct RowCfg {
 typedef __attribute__((ext_vector_type(2))) int i32x2_t;
 typedef __attribute__((address_space(3))) i32x2_t lds_i32x2_t;
 
-// eight e4m3 numbers as bf16 (exact)
-__device__ __forceinline__ bf16x8_t fp8_to_bf16(unsigned w0, unsigned w1) {
-  const bf16x2_t p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true)};
+// A block's scale as power * rest: the conversion of its codes takes the power of two along (exact, down to the smallest bf16 numbers), so that neither a
+// product with the queries nor a weight leaves the range of its type where the rows themselves do not.  The rest goes into logits and weights: 1 for
+// the powers of two that are written here, within (-4, 4) for any scale.
+struct BlockScale { float power, rest; };
+__device__ __forceinline__ BlockScale block_scale(int bits) {
+  const int e = min(max(bits >> 23 & 255, 7), 253);
+  return {__int_as_float(e << 23), __int_as_float(bits) * __int_as_float((254 - e) << 23)};
+}
+
+// eight e4m3 numbers times a power of two as bf16
+__device__ __forceinline__ bf16x8_t fp8_to_bf16(unsigned w0, unsigned w1, float power) {
+  const bf16x2_t p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, power, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, power, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, power, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, power, true)};
   bf16x8_t v;
   __builtin_memcpy(&v, p, 16);
   return v;
@@ -148,10 +157,10 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
   }
   for (; r0 < s1; r0 += step) {
     const bool more = r0 + step < s1;
-    float kscale = 1.f, vscale = 1.f;
+    BlockScale kscale, vscale;
     if constexpr (R == kRowFp8) {
-      kscale = __int_as_float(scalar_ints(reinterpret_cast<const int *>(a.k_scales))[scale_at + r0 / kQuantRows]);
-      vscale = __int_as_float(scalar_ints(reinterpret_cast<const int *>(a.v_scales))[scale_at + r0 / kQuantRows]);
+      kscale = block_scale(scalar_ints(reinterpret_cast<const int *>(a.k_scales))[scale_at + r0 / kQuantRows]);
+      vscale = block_scale(scalar_ints(reinterpret_cast<const int *>(a.v_scales))[scale_at + r0 / kQuantRows]);
     }
     wait_loads<kVLoads>();  // the K tile is there, the V tile may still be on its way
     uint4 kf[SUBS][KJ];
@@ -183,7 +192,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
           __builtin_memcpy(&k, &c, 16);
           sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qb[j][0], sc, 0, 0, 0);
         } else {
-          const bf16x8_t k0 = fp8_to_bf16(c.x, c.y), k1 = fp8_to_bf16(c.z, c.w);
+          const bf16x8_t k0 = fp8_to_bf16(c.x, c.y, kscale.power), k1 = fp8_to_bf16(c.z, c.w, kscale.power);
 #pragma unroll
           for (int t = (QBF16 ? 1 : 3) - 1; t >= 0; --t) {
             sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qb[2 * j][t], sc, 0, 0, 0);
@@ -195,7 +204,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
     }
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
-      if constexpr (R == kRowFp8) p[u] *= kscale;
+      if constexpr (R == kRowFp8) p[u] *= kscale.rest;
       if (a.score.cap > 0.f) {
         if (!QBF16 || a.score.fine) {
 #pragma unroll
@@ -238,7 +247,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
       for (int i = 0; i < 4; ++i) {
         p[u][i] = fast_exp2(p[u][i] - m);
         z += p[u][i];
-        if constexpr (R == kRowFp8) p[u][i] *= vscale;
+        if constexpr (R == kRowFp8) p[u][i] *= vscale.rest;
       }
     if (more) wait_loads<kKLoads>(); else wait_loads<0>();  // the V tile is there
     const int left = s1 - r0 - 4 * q4;  // this lane's key i (of the second half: 16 + i) is a row while i < left
@@ -323,7 +332,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
       }
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
-        const bf16x8_t v = fp8_to_bf16((unsigned)vf[t][0], (unsigned)vf[t][1]);
+        const bf16x8_t v = fp8_to_bf16((unsigned)vf[t][0], (unsigned)vf[t][1], vscale.power);
 #pragma unroll
         for (int k = 0; k < kTerms; ++k) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pk[k], acc[t], 0, 0, 0);
       }

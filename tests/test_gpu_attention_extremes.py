@@ -176,3 +176,39 @@ def test_prompt_layouts_of_its_own(dtype, d, hq, hkv, lens, window):
     a.p = fb.Params(2, hq, hkv, d, dtype, lens, lens, a.spans, window, 0.25, [1.0] * len(lens), k_strides=(hkv * T * d, T * d, d))
     a.run()
     a.check(f"{dtype} {d} {hq}/{hkv} {lens} window {window}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k_size, q_size, v_size", [(1.0, 1.0, 2.0 ** -117), (2.0 ** -113, 2.0 ** 119, 1.0), (2.0 ** 100, 2.0 ** -100, 2.0 ** 118), (1.0, 1.0, 2.0 ** -60)])
+def test_rows_in_8_bits_of_any_magnitude(dtype, k_size, q_size, v_size):
+    """Blocks of tiny and of huge numbers: the logits and the outputs are those of rows of ordinary size, scaled."""
+    lens = [300, 33]
+    a = Attention("fp8", dtype, 1, 4, 2, 64, lens, scale=0.125 / (k_size * q_size), seed=17)
+    a.q = (a.q.double() * q_size).to(a.q.dtype)
+    a.K, a.V = ((x.double().clamp(-60, 60) * s).to(x.dtype) for x, s in ((a.K, k_size), (a.V, v_size)))
+    upload(a)
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu()
+    K, V = a.values()
+    for b, n in enumerate(lens):
+        r = slice(a.cu[b], a.cu[b] + n)
+        for h in range(4):
+            want, tol = ref.attend(a.q[0, h, b][None], K[0, h // 2, r], V[0, h // 2, r] / v_size, a.scale, 0.0, None, None, None, DT[dtype], 2.0 ** -15 if dtype == "bf16" else 0.0)
+            ref.check(got[0, h, b][None].double() / v_size, want, tol, (b, h))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_in_8_bits_at_any_scale(dtype, d):
+    """Scales that the library does not write: no powers of two, negative ones, 0, subnormal ones."""
+    lens = [310, 64]
+    a = Attention("fp8", dtype, 1, 4, 2, d, lens, scale=1.0, seed=18)
+    g = torch.Generator().manual_seed(19)
+    for scales, size in ((a.cache.k_scales, 2.0 ** -8), (a.cache.v_scales, 0.01)):
+        some = torch.tensor([0.3712, -1.7, 0.0, 1.0, 1.99999, 1e-36, -1e-40, 0.75]) * size
+        scales.copy_(some[torch.randint(0, len(some), scales.shape, generator=g)])
+    for codes in (a.cache.k_codes, a.cache.v_codes):
+        codes.view(torch.uint8).copy_(torch.randint(0, 256, codes.shape, generator=g, dtype=torch.uint8) & 0xbf)  # (numbers of up to 1.875)
+    a.run()
+    a.check(f"{dtype} {d} any scale")
