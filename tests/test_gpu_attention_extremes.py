@@ -212,3 +212,56 @@ def test_rows_in_8_bits_at_any_scale(dtype, d):
         codes.view(torch.uint8).copy_(torch.randint(0, 256, codes.shape, generator=g, dtype=torch.uint8) & 0xbf)  # (numbers of up to 1.875)
     a.run()
     a.check(f"{dtype} {d} any scale")
+
+
+def watched(units, L, d):
+    """V in which channel c of unit g is 1 in row g * d + c alone: every row of L <= units * d has a channel of its own."""
+    v = torch.zeros(units, L, d)
+    r = torch.arange(L)
+    v[r // d, r, r % d] = 1.0
+    return v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq, hkv, L, masks", [(8, 8, 1000, False), (40, 8, 1000, False), (34, 17, 2100, False), (8, 8, 1000, True), (40, 8, 1000, True), (34, 17, 2100, True)])
+def test_every_key_of_a_prompt_counts_once(dtype, hq, hkv, L, masks):
+    """All keys weigh the same, so that every output is 1 / their number where the row sees the channel's key, and 0 where it does not."""
+    d, G = 128, hq // hkv
+    spans = [[(0, 100, 0), (100, 333, 1), (333, 700, 0), (700, 790, 1), (790, L, 0)]]
+    a = Prompt(dtype, 1, hq, hkv, d, [L], spans=spans, prefix=[57] if masks else None, image_spans=masks, seed=29)
+    a.Q[:] = 0.0
+    a.V[0] = watched(hkv, L, d).to(DT[dtype])
+    a.upload()
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu().double()[0]
+    seen = (~a.hidden(0)).double()
+    want = seen / seen.sum(-1, keepdim=True)
+    tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * 1.001 * want  # the result's rounding; fp32: that of 1 / z before it as well
+    for h in range(hq):
+        keys = slice(h // G * d, min(L, h // G * d + d))
+        n = keys.stop - keys.start
+        if n > 0:
+            assert ((got[h, :, :n] - want[:, keys]).abs() <= tol[:, keys]).all(), h
+            assert (got[h, :, n:] == 0).all()
+
+
+@pytest.mark.parametrize("rows, dtype", KINDS)
+@pytest.mark.parametrize("hkv, G, lens", [(8, 1, [1000]), (8, 3, [257, 31, 640]), (40, 2, [2500]), (64, 1, [1, 700, 16, 900, 33]), (16, 17, [1100, 5])])
+def test_every_row_of_a_cache_counts_once(rows, dtype, hkv, G, lens):
+    d = 64
+    a = Attention(rows, dtype, 1, hkv * G, hkv, d, lens, seed=30)
+    a.q[:] = 0.0
+    a.V[:] = 0.0
+    for b, n in enumerate(lens):
+        m = min(n, hkv * d)
+        a.V[0, :, a.cu[b]:a.cu[b] + m] = watched(hkv, m, d).to(DT[dtype])
+    upload(a)
+    a.run()
+    torch.cuda.synchronize()
+    got = a.out.cpu().double()[0]
+    for b, n in enumerate(lens):
+        there = (torch.arange(hkv * d) < n).double().view(hkv, d) / n
+        want = there.repeat_interleave(G, 0)
+        # the result's rounding; fp32: that of the quotient and, beside codes, of none of the terms (weights are 1)
+        assert ((got[:, b] - want).abs() <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * 1.001 * want).all(), b
