@@ -90,7 +90,7 @@ __global__ __launch_bounds__(WAVES * 64, R == kRowF32 ? 2 : 4) void cache_attent
   constexpr int NCH = RC::NCH, TR = RC::kRows, SUBS = RC::kSubs, DT = D / 16;
   constexpr int kKLoads = RC::kLoads + (POS ? 1 : 0), kVLoads = RC::kLoads;
   constexpr int kTerms = QBF16 ? 2 : 3;  // of p
-  constexpr int KJ = R == kRowF32 ? NCH / 4 : R == kRowBF16 ? NCH / 4 : NCH / 4;  // chunks of a row in a lane
+  constexpr int KJ = NCH / 4;  // chunks of a row in a lane
   extern __shared__ __align__(16) uint4 lds_rows[];  // [waves] K tile, V tile, positions; at the end the waves' states
   const DecodeTask task = decode_task<ORDERED>(a);
   const int b = task.b, x = task.x, gkv = task.gkv, l = task.l, len = task.B, s0 = task.s0, s1 = task.s1;

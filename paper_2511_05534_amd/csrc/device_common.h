@@ -431,13 +431,13 @@ __device__ __forceinline__ int lane_id_here() {
 // padding, so that one chunk column of 16 consecutive rows falls on 16 different 16-byte columns of the banks.
 // The permutation touches the two low bits of the chunk number only: a lane needs two base addresses, for
 // even and odd fragments, and everything else is an immediate offset.
-template <bool BF16, int D, int ROWS = Cfg<BF16, D>::NCH == 32 ? 64 : 128>
+template <bool BF16, int D>
 struct KeyTile {
   static constexpr int NCH = Cfg<BF16, D>::NCH;
   static_assert(NCH == 8 || NCH == 16 || NCH == 32, "rows of 128, 256 or 512 bytes");
   static constexpr int kGroup = 64 / NCH;
   static constexpr int kGroupChunks = 64 + (NCH == 32 ? 2 : 4);
-  static constexpr int kRows = ROWS;
+  static constexpr int kRows = NCH == 32 ? 64 : 128;
   static constexpr int kChunks = kRows / kGroup * kGroupChunks;
   __device__ static __forceinline__ int permute(int row_in_group) { return NCH == 8 ? row_in_group >> 1 : row_in_group; }
   // bytes from a tile's start to chunk 2 * odd + half of row n (n < 32); fragment f of block kb of 32 rows lies
