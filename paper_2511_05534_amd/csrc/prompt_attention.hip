@@ -32,9 +32,11 @@ namespace flowmm {
 namespace {
 
 constexpr int kPThreads = kPromptWaves * 64;
-// Workgroups of a group of units: as many as compute units, so that the workgroups of a unit run together and its keys and values are fetched once (a unit stays on an XCD).
-// Groups of 8 units / 128 workgroups / 256 / 512 / 1024 / 4096, us: 256 units x 2048 tokens 407 / 362 / 350 / 348 / 367 / 387, 512 x 1100 300 / 296 / 308 / 316 / 331 / 338, 1024 x 400
-// 184 / 157 / 163 / 172 / 173 / 173, 112 x 675 (28/4 heads) 182 / 182 / 181 / 183 / 190 / 195; 8 units of 16384 tokens the same throughout.
+// Units of a group: as many as have a workgroup for every compute unit, so that the workgroups of a unit run together and its keys and values are fetched once (a unit stays
+// on an XCD), in fours for every XCD: with fewer, and with few units left for the last group, rows as late as each other meet on an XCD's compute units less evenly.
+// All units together / groups of this size in eights / in 32s, us: 256 units x 2048 tokens 372 / 339 / 344, 512 x 1100 330 / 303 / 294, 1024 x 400 164 / 155 / 155, 112 x 675
+// (28/4 heads) 188 / 178 / 180, 32 x 3000 93 / 119 / 92, 128 x 1100 79 / 89 / 76, 32 x 8 sequences of 1000 118 / 150 / 118, 32 x 4 of 2000 171 / 218 / 171; 128 x 675, in 96 and 32,
+// 39 / 42 / 42; up to 32 units, or 8 of 16384 tokens, the first and the last are the same.
 constexpr int kPromptGroupWgs = 256;
 
 // V rows in LDS: whole rows by direct loads as in KeyTile, the chunks of a row permuted so that the four rows that 16 lanes transpose, 32 bytes
@@ -517,8 +519,8 @@ hipError_t launch_prompt_attention(const PromptArgs &args, const int *words, int
   const int units = a.n_layers * a.Hkv;
   const long long grid = (long long)units * a.wgs_total;
   if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  a.group = (kPromptGroupWgs / a.wgs_total + 7) / 8 * 8;
-  if (a.group < 8) a.group = 8;
+  a.group = (kPromptGroupWgs / a.wgs_total + 31) / 32 * 32;
+  if (a.group < 32) a.group = 32;
   if (a.group > units) a.group = units;
   KernelArgs<PromptArgs> k;
   fill_kernel_args(k, a, words, n_words);
