@@ -244,9 +244,11 @@ flowmm_status flowmm_cache_remerge(const flowmm_params *p, const int32_t *cu_cap
  * For query head h, the query at position i and the key at position j of its sequence:
  *   x = scale * <q, k>;  cap > 0: x = cap * tanh(x / cap);  slopes: x = x - slopes[h] * |i - j|.
  * prefix and image_spans are read by flowmm_prompt_attention, row_pos and q_pos by the two cache
- * attentions (which need both or neither).  A query all of whose logits are -infinity gets NaN, 0 / 0, as
- * from flowmm_decode_attention; logits of 2^127 and more may count as infinite.  The sums over the keys of weights
- * (1 at the most) times V are fp32 numbers: V times the number of keys has to stay within their range. */
+ * attentions (which need both or neither).  cap * tanh(x / cap) is within 2^-20 of the cap (fp32 calls and
+ * caps above 512: within 2^-21 of itself where |x| is below a quarter of the cap).  A query all of whose
+ * logits are -infinity gets NaN, 0 / 0, as from flowmm_decode_attention; logits of 2^127 and more may count
+ * as infinite.  The sums over the keys of weights (1 at the most) times V are fp32 numbers: V times the
+ * number of keys has to stay within their range. */
 typedef struct {
   float cap;              /* within [0, 2^120], scale / cap as well; 0: no cap */
   const float *slopes;    /* device [Hq], or NULL: no bias */

@@ -12,7 +12,7 @@
 //               codes: 16 of them, two v_mfma 16x16x32 after v_cvt_scalef32_pk_bf16_fp8 with the block's scale (exact); fp32 queries as three bf16 terms
 //               bf16 : 8 channels, one 16x16x32;  fp32: 4 channels, four 16x16x4
 //   scores  : scale, cap, bias by distance in fp32, log2 domain
-//   output  : O[channel][head] += V^T x p, p at the accuracy of the result: the two leading bf16 terms (2^-16) for bf16 results, three
+//   output  : O[channel][head] += V^T x p, p at the accuracy of the result: the two leading bf16 terms (short of 2^-15) for bf16 results, three
 //             for fp32 ones, fp32 itself beside fp32 rows.  V comes out of LDS transposed
 //             (ds_read_b64_tr_b8, _tr_b16), in the order of keys in which the accumulators of S hold p.
 // Rows past a sequence's end are read as its last one; their p is 0 and so are their V, whatever that row holds.

@@ -970,10 +970,12 @@ flowmm_status quantize_call(const flowmm_params *p, const int32_t *cu_capacity, 
 }
 
 // Waves that share the query rows of the prompt's attention and split the keys, `items` being the groups of 32 rows (all heads, layers): one workgroup of eight waves has a
-// compute unit to itself.  Causal prompts end with short rows that fill gaps, so that the split is worth it up to twice the compute units (bf16, 128 channels, us in
-// one / two / four: 704 items of 675 tokens 26 / 17 / 18, 1216 of 1200 38 / 25 / 37, 2016 of 2000 59 / 46 / 72, 3008 of 3000 92 / 95 / 141; fp32, whose rounds
-// cost what they compute, 1024 of 1000 279 / 163 / 115, 1600 of 1600 450 / 247 / 278, 3008 of 3000 839 / 793 / 861).  Rows that nearly all see as much (a prefix or a picture
-// of most of the prompt) take as many rounds as there are: 704 items of 675 tokens, 576 of them a picture, 27 / 21 / 27, 1216 of 1200 42 / 53 / 57, 2016 of 2000 76 / 88 / 121.
+// compute unit to itself.  Causal prompts end with short rows that fill gaps, so that the split is worth it up to twice the compute units, and less and less beyond (bf16, 128 channels, us
+// in one / two / four: 512 items of 512 tokens 20.9 / 14.4 / 12.4, 704 of 675 27.0 / 17.6 / 17.3, 1024 of 1000 34.7 / 22.6 / 25.6, 2016 of 2000 60 / 46 / 74, 2528 of 2500 76 / 73 / 109,
+// 3008 of 3000 92 / 96 / 144; 64 channels 2016 42 / 31 / 37, 2304 48 / 41 / 45, 2816 57 / 56 / 63; fp32, whose rounds cost what they compute, 1024 of 1000 283 / 164 / 116, 1408 of 1400
+// 400 / 222 / 227, 1600 of 1600 452 / 251 / 280, 3008 of 3000 846 / 807 / 876, 3616 of 3600 1077 / 1095 / 1287).  Rows that nearly all see as much (a prefix or a picture of most of the
+// prompt) take as many rounds as there are: 704 items of 675 tokens, 576 of them a picture, 27 / 20 / 27, 1216 of 1200 41 / 49 / 58, 2016 of 2000 65 / 77 / 110, 2304 of 2300 82 / 88 / 133;
+// fp32 704 201 / 115 / 138, 1216 345 / 342 / 331.
 int prompt_key_split(const flowmm_params *p, const int32_t *prefix, int image_spans, const Shape &sh, long long items) {
   if (items > 512 && items < 2048 && (prefix || image_spans)) {
     long long sum = 0, n = 0, most = 0;

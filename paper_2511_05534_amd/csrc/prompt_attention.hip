@@ -17,7 +17,7 @@
 // the picture is the last one.  The loads cost nothing that shows (all from one tile: 3 % less).  Blocks that some rows see in part take the same path with a mask, two at
 // a time as well (one by one, each of V's numbers filtered: 675 tokens with a picture 25.4 us).
 //
-// bf16: P is rounded to bf16 for the second product, as V is one (relative 2^-9 a weight, each its own, so that it stays below the
+// bf16: P is rounded to bf16 for the second product, as V is one (by 2^-8 of a weight at the most, each its own, so that it stays below the
 // rounding of the result wherever many keys count); its sum is of the fp32 weights.  fp32: both products by the fp32 matrix instructions.
 #include <cfloat>
 #include <type_traits>
