@@ -301,6 +301,8 @@ class QuantizedCache:
                 raise ValueError(f"a {dtype} tensor of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
         if k.stride() != v.stride() or k.stride(-1) != 1 or not ks.is_contiguous() or not vs.is_contiguous():
             raise ValueError("k_codes and v_codes share their strides, their last dimension and the scales are contiguous")
+        if k.device.type != "cuda" or any(t.device != k.device for t in (v, ks, vs)):
+            raise ValueError("codes and scales lie on one GPU")
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k, v, ks, vs
         self.c = flowmm_quantized_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), *k.stride()[:3])
 

@@ -198,3 +198,19 @@ def test_prompt_attention_takes_layouts_that_the_plan_refuses():
 def test_the_last_error_is_that_of_a_call_that_failed():
     refused(lambda: fb.flowmm_prompt_attention(params(window=0), None, good, far[0], far[1], (4 * 90 * 128, 90 * 128, 128), far[2], far[3], BIG), "window")
     refused(lambda: fb.flowmm_prompt_attention(params(n_q_heads=48), None, good, far[0], far[1], (48 * 90 * 128, 90 * 128, 8), far[2], far[3], BIG), "head_dim")
+
+
+def test_a_cache_in_8_bits_lies_on_a_gpu():
+    """Tensors of the host's memory, whose addresses mean nothing to the kernels, and of the wrong shape, type or order."""
+    import torch
+    p = params()
+
+    def tensors(codes=(2, 2, 90, 128), scales=(2, 2, 4), dtype=torch.float8_e4m3fn, order=lambda t: t):
+        return [order(torch.zeros(codes, dtype=torch.uint8).view(dtype)) for _ in range(2)] + [torch.zeros(scales) for _ in range(2)]
+
+    for kw, word in ((dict(), "GPU"), (dict(codes=(2, 2, 89, 128)), "shape"), (dict(scales=(2, 2, 3)), "shape"), (dict(dtype=torch.uint8), "float8"),
+                     (dict(codes=(2, 2, 128, 90), order=lambda t: t.transpose(2, 3)), "contiguous")):
+        with pytest.raises(ValueError, match=word):
+            fb.QuantizedCache(p, CAP, tensors=tensors(**kw))
+    with pytest.raises(ValueError, match="GPU"):
+        fb.QuantizedCache(p, CAP, "cpu")
