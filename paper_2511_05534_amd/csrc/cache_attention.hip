@@ -46,10 +46,10 @@ typedef __attribute__((address_space(3))) i32x2_t lds_i32x2_t;
 
 // A block's scale as power * rest: the conversion of its codes takes the power of two along (exact, down to the smallest bf16 numbers), so that neither a
 // product with the queries nor a weight leaves the range of its type where the rows themselves do not.  The rest goes into logits and weights: 1 for
-// the powers of two that are written here, within (-4, 4) for any scale.
+// the powers of two that are written here, but 2 for the largest, 2^120, which would bring codes from 256 on (numbers that e4m3 rounded up, beyond the largest float) to infinity.
 struct BlockScale { float power, rest; };
 __device__ __forceinline__ BlockScale block_scale(int bits) {
-  const int e = min(max(bits >> 23 & 255, 7), 253);
+  const int e = min(max(bits >> 23 & 255, 7), 246);  // 2^-120 .. 2^119
   return {__int_as_float(e << 23), __int_as_float(bits) * __int_as_float((254 - e) << 23)};
 }
 

@@ -214,6 +214,25 @@ def test_rows_in_8_bits_at_any_scale(dtype, d):
     a.check(f"{dtype} {d} any scale")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("below", [1000.0, 60.0])
+def test_codes_that_stand_for_more_than_the_largest_float(dtype, below):
+    """The largest numbers, which e4m3 rounds up to 2^128, in rows that weigh 0, or exp(-60)."""
+    lens = [90, 700]
+    a = Attention("fp8", dtype, 1, 4, 2, 64, lens, scale=0.125, seed=31)
+    a.q[:] = 0.0
+    a.q[..., 0] = 8.0
+    a.K[:] = 0.0
+    for b, n in enumerate(lens):
+        far = torch.arange(a.cu[b] + 5, a.cu[b] + n, 64)
+        a.K[:, :, far, 0] = -below
+        a.V[:, :, far] = torch.finfo(a.V.dtype).max
+    upload(a)
+    a.run()
+    assert float(a.cache.v_scales.max()) == 2.0 ** 120 and float(a.values()[1].max()) == 2.0 ** 128
+    a.check(f"{dtype} below {below}")
+
+
 def watched(units, L, d):
     """V in which channel c of unit g is 1 in row g * d + c alone: every row of L <= units * d has a channel of its own."""
     v = torch.zeros(units, L, d)
