@@ -315,8 +315,8 @@ flowmm_status flowmm_cache_quantize(const flowmm_params *p, const int32_t *cu_ca
                                     const int32_t *cu_rows, const void *K_rows, const void *V_rows,
                                     const flowmm_quantized_cache *cache, void *stream);
 
-/* The way back, for a re-merge: rows code * scale, rounded to nearest-even in the dtype of p; here
- * sequences must not share rows. */
+/* The way back, for a re-merge: rows code * scale, rounded to nearest-even in the dtype of p (numbers from
+ * 3.3e38 on, whose codes were rounded up to 2^128, come back as infinities); here sequences must not share rows. */
 flowmm_status flowmm_cache_dequantize(const flowmm_params *p, const int32_t *cu_capacity, const int32_t *lengths,
                                       const int32_t *cu_rows, const flowmm_quantized_cache *cache, void *K_rows,
                                       void *V_rows, void *stream);
