@@ -1004,7 +1004,7 @@ flowmm_status prompt_layout(const flowmm_params *p, Layout &lo, size_t workspace
   char message[sizeof(g_err)];
   std::memcpy(message, g_err, sizeof(g_err));
   const flowmm_status refused = build_layout(p, lo, workspace_bytes);
-  if (refused == FLOWMM_OK || !p || p->batch < 1 || !p->budget_tokens || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) return refused;
+  if (refused == FLOWMM_OK || !p || p->batch < 1 || !p->cu_seqlens || !p->budget_tokens || !p->spans || !p->cu_spans || !p->tau || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) return refused;
   if (p->n_q_heads > 1024) return fail(FLOWMM_EUNSUPPORTED, "more than 1024 query heads");
   const std::vector<int32_t> ones((size_t)p->batch, 1);
   flowmm_params plain = *p;

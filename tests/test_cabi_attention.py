@@ -214,3 +214,12 @@ def test_a_cache_in_8_bits_lies_on_a_gpu():
             fb.QuantizedCache(p, CAP, tensors=tensors(**kw))
     with pytest.raises(ValueError, match="GPU"):
         fb.QuantizedCache(p, CAP, "cpu")
+
+
+def test_prompt_attention_without_its_arrays():
+    """Refused before anything of the batch's size is allocated."""
+    for name in ("cu_seqlens", "budget_tokens", "spans", "cu_spans", "tau"):
+        p = params(n_q_heads=48)
+        setattr(p.c, name, None)
+        p.c.batch = 2 ** 31 - 1
+        refused(lambda: fb.flowmm_prompt_attention(p, None, good, far[0], far[1], (48 * 90 * 128, 90 * 128, 128), far[2], far[3], BIG), "NULL")
