@@ -33,10 +33,12 @@ namespace {
 
 constexpr int kPThreads = kPromptWaves * 64;
 // Units of a group: as many as have a workgroup for every compute unit, so that the workgroups of a unit run together and its keys and values are fetched once (a unit stays
-// on an XCD), in fours for every XCD: with fewer, and with few units left for the last group, rows as late as each other meet on an XCD's compute units less evenly.
-// All units together / groups of this size in eights / in 32s, us: 256 units x 2048 tokens 372 / 339 / 344, 512 x 1100 330 / 303 / 294, 1024 x 400 164 / 155 / 155, 112 x 675
-// (28/4 heads) 188 / 178 / 180, 32 x 3000 93 / 119 / 92, 128 x 1100 79 / 89 / 76, 32 x 8 sequences of 1000 118 / 150 / 118, 32 x 4 of 2000 171 / 218 / 171; 128 x 675, in 96 and 32,
-// 39 / 42 / 42; up to 32 units, or 8 of 16384 tokens, the first and the last are the same.
+// on an XCD), in fours for every XCD, and those that are left over spread over the groups: with fewer units at a time rows as late as each other meet on an XCD's compute units
+// less evenly.
+// All units together / groups in eights, the rest behind them / these, us: 256 units x 2048 tokens 372 / 339 / 344, 512 x 1100 330 / 303 / 294, 1024 x 400 164 / 155 / 155, 112 x 675
+// (28/4 heads) 188 / 178 / 183, 32 x 3000 93 / 119 / 92, 128 x 1100 79 / 89 / 76, 32 x 8 sequences of 1000 118 / 150 / 118, 32 x 4 of 2000 171 / 218 / 171; all together / in 32s, the rest
+// behind them / these: 40 x 3000 111 / 156 / 111, 36 x 675 20 / 26 / 20, 72 x 2000 103 / 138 / 102, 128 x 675 40 / 43 / 40, 112 x 3000 (32/8) 1172 / 1131 / 1154; 8 units of 16384 tokens
+// are one group.
 constexpr int kPromptGroupWgs = 256;
 
 // V rows in LDS: whole rows by direct loads as in KeyTile, the chunks of a row permuted so that the four rows that 16 lanes transpose, 32 bytes
@@ -521,7 +523,8 @@ hipError_t launch_prompt_attention(const PromptArgs &args, const int *words, int
   if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   a.group = (kPromptGroupWgs / a.wgs_total + 31) / 32 * 32;
   if (a.group < 32) a.group = 32;
-  if (a.group > units) a.group = units;
+  const int groups = units / a.group;
+  a.group = groups > 1 ? ((units + groups - 1) / groups + 7) / 8 * 8 : units;
   KernelArgs<PromptArgs> k;
   fill_kernel_args(k, a, words, n_words);
   if (a.bf16) return a.d == 128 ? launch_prompt_d<true, 128>(k, (unsigned)grid, stream) : launch_prompt_d<true, 64>(k, (unsigned)grid, stream);

@@ -284,3 +284,19 @@ def test_every_row_of_a_cache_counts_once(rows, dtype, hkv, G, lens):
         want = there.repeat_interleave(G, 0)
         # the result's rounding; fp32: that of the quotient and, beside codes, of none of the terms (weights are 1)
         assert ((got[:, b] - want).abs() <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * 1.001 * want).all(), b
+
+
+@pytest.mark.parametrize("dtype, layers, hq, hkv, L", [("bf16", 1, 36, 36, 2100), ("bf16", 1, 72, 72, 2100), ("bf16", 10, 16, 8, 1500), ("f32", 4, 17, 17, 3700), ("bf16", 9, 10, 10, 40)])
+def test_units_in_groups(dtype, layers, hq, hkv, L):
+    """More (layer, kv head) units than a group takes, in numbers that do not divide: every row of every head, the mean of what it sees."""
+    a = Prompt(dtype, layers, hq, hkv, 64, [L], seed=32)
+    a.Q[:] = 0.0
+    a.upload()
+    a.run()
+    torch.cuda.synchronize()
+    got, seen = a.out.double(), torch.arange(1, L + 1, dtype=torch.float64, device=DEV)[:, None]
+    V = a.dev[1].double().repeat_interleave(hq // hkv, 1)
+    want, size = V.cumsum(2) / seen, V.abs().cumsum(2) / seen
+    # the result's rounding and the sum's (weights are 1: exact)
+    tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * want.abs() + L * 2.0 ** -24 * size
+    assert ((got - want).abs() <= tol).all()
